@@ -344,8 +344,9 @@ def _run_own(st):
         C.ec2moe_gate_logits(st["desc"], t["X"], t["W_local"], t["b_local"], t["W_global"], t["b_global"], st["Y"], ws,
                              ws.numel())
         return st["Y"]
-    C.ec2moe_balance_loss(st["desc"], t["logits"], st["mask"], t["topk_idx"], t["valid"], t["segments"], st["segments"],
-                          0.01, t["d_loss"], st["loss"], st["counts"], st["d_logits"], st["d_bias"], ws, ws.numel())
+    C.ec2moe_balance_loss(st["desc"], t["logits"], t["logits"].shape[1], st["mask"], t["topk_idx"], t["valid"],
+                          t["segments"], st["segments"], 0.01, t["d_loss"], st["loss"], st["counts"], st["d_logits"],
+                          st["d_bias"], ws, ws.numel())
     return {n: st[n] for n in ("loss", "counts", "d_logits", "d_bias")}
 
 
