@@ -279,7 +279,9 @@ ec2moe_status ec2moe_layer_forward(const ec2moe_layer_desc* desc, const ec2moe_l
  * tensor-core kernel gave up; EC2MOE_ERR_INVALID_ARG when a routing kernel met
  * (and skipped) an expert id outside [0, E) in a caller's topk_idx, or a
  * grouped expert GEMM met (and skipped) a group range in `offsets` outside
- * [0, T * k] or a destination in `perm` outside [0, T * k); EC2MOE_ERR_CUDA
+ * [0, T * k] or a destination in `perm` outside [0, T * k), or one of the 8-bit
+ * and balance entry points an entry that its description names;
+ * EC2MOE_ERR_CUDA
  * when the stream reports an error.  A timeout takes precedence. */
 ec2moe_status ec2moe_last_device_error(ec2moe_stream_t stream);
 
@@ -331,6 +333,140 @@ ec2moe_status ec2moe_layer_forward_pipelined(const ec2moe_layer_desc* desc, cons
                                              size_t ws_bytes, int32_t n_micro, ec2moe_stream_t stream_end,
                                              ec2moe_stream_t stream_cloud);
 
+/* ---------------------------------------------------------------------------
+ * Experts in 8-bit floating point.  Values are e4m3 (1 sign, 4 exponent, 3
+ * mantissa bits, largest 448, no infinities), one byte each, with one fp32 scale
+ * for each block of EC2MOE_FP8_BLOCK columns: a stored value q stands for q times
+ * its block's scale.  Activations have a scale per row and block
+ * ([rows, ceil(cols / 128)]), weights one per 128 x 128 block
+ * ([mats, ceil(rows / 128), ceil(cols / 128)]); scales are any fp32 numbers, not
+ * only those of ec2moe_fp8_quantize.  Rows are dense and multiples of 16 bytes
+ * (cols, d, d_ff multiples of 16; others return EC2MOE_ERR_MISALIGNED); a last
+ * block may be narrower than 128.  The paper has no counterpart: its experts
+ * (Eq. 1) are computed from rounded inputs here, with fp32 sums. */
+#define EC2MOE_FP8_BLOCK 128
+
+/* X (dtype; rows of pitch ld >= cols elements) to e4m3 Q (dense) and its scales:
+ *   a = max(2^-96, max |x| over the block), scale = a / 448, q = e4m3(x * (448 / a))
+ * rounded to nearest, ties to even.  A NaN becomes e4m3's NaN and does not count
+ * for its block's scale; an infinity makes its block's scale infinite.
+ *  n_mats, rows  matrices of `rows` rows each, one behind the other in X and Q
+ *  block_rows    1: a scale per row and 128 columns; 128: per 128 x 128 block,
+ *                blocks starting anew in each matrix
+ *  inv_perm, k   NULL and 0, or (block_rows = 1, n_mats = 1) device int32
+ *                [rows, k] of ec2moe_route, 1 <= k <= EC2MOE_MAX_TOPK: row t is
+ *                written to the rows inv_perm[t * k + s], s < k, of Q
+ *                [rows * k, cols] and scale.  An entry of -1 is skipped; another
+ *                one outside [0, rows * k) too, and ec2moe_last_device_error then
+ *                reports EC2MOE_ERR_INVALID_ARG.
+ * No rows is a no-op. */
+ec2moe_status ec2moe_fp8_quantize(int32_t dtype, int32_t n_mats, int32_t rows, int32_t cols, int64_t ld,
+                                  const void* X, int32_t block_rows, const int32_t* inv_perm, int32_t k, void* Q,
+                                  float* scale, ec2moe_stream_t stream);
+
+/* Bytes of device workspace ec2moe_fp8_gemm needs (0: none, or an invalid size). */
+size_t ec2moe_fp8_gemm_workspace_size(int32_t n_groups, int32_t rows, int32_t N, int32_t K);
+
+/* C_g = A_g B_g^T of 8-bit operands: group g owns the rows [offsets[g],
+ * offsets[g + 1]) of A [rows, K] and of C, and the weights B[g] [N, K].
+ *  A_scale   fp32 [rows, ceil(K / 128)]
+ *  offsets   device int32 [n_groups + 1], or NULL with n_groups = 1: all rows
+ *  B_scale   fp32 [n_groups, ceil(N / 128), ceil(K / 128)]
+ *  out_dtype EC2MOE_BF16 or EC2MOE_F32: type of C, rows of pitch ldc >= N
+ *            elements (a multiple of 16 bytes)
+ * Every block's products are summed in fp32 and the scaled sums of the blocks
+ * added in fp32, rounded once to the output.  Rows of no group are not written; a
+ * group whose range is not inside [0, rows] is skipped and
+ * ec2moe_last_device_error then reports EC2MOE_ERR_INVALID_ARG.  No rows is a
+ * no-op. */
+ec2moe_status ec2moe_fp8_gemm(int32_t n_groups, int32_t rows, int32_t N, int32_t K, const void* A,
+                              const float* A_scale, const int32_t* offsets, const void* B, const float* B_scale,
+                              int32_t out_dtype, void* C, int64_t ldc, void* workspace, size_t ws_bytes,
+                              ec2moe_stream_t stream);
+
+/* Expert weights in e4m3 with 128 x 128 scales, shapes as in ec2moe_layer_weights
+ * (W3, S3 NULL for GELU): W1, W3 [E, d_ff, d], S1, S3 [E, ceil(d_ff / 128),
+ * ceil(d / 128)]; W2 [E, d, d_ff], S2 [E, ceil(d / 128), ceil(d_ff / 128)]. */
+typedef struct ec2moe_fp8_weights {
+  const void* W1;
+  const float* S1;
+  const void* W3;
+  const float* S3;
+  const void* W2;
+  const float* S2;
+} ec2moe_fp8_weights;
+
+/* Bytes of device workspace ec2moe_experts_fp8 needs (hidden rows and scales). */
+size_t ec2moe_experts_fp8_workspace_size(const ec2moe_layer_desc* desc);
+
+/* ec2moe_experts on 8-bit rows and weights.
+ * Passage: Eq. 1, each term G(x)_i E_i(x).
+ *  Xq, Xs    e4m3 [T * k, d] rows in expert order and their scales
+ *            (ec2moe_fp8_quantize with the inv_perm of ec2moe_route)
+ *  slot_out  out [T * k, d] in desc->dtype: slot_out[t * k + s] =
+ *            topk_w[t, s] * E_e(x_t) for e = topk_idx[t, s]
+ * The hidden rows are the activation of the fp32 sums, quantised like
+ * ec2moe_fp8_quantize's rows.  offsets, perm, topk_w and what happens to entries
+ * out of range as for ec2moe_experts. */
+ec2moe_status ec2moe_experts_fp8(const ec2moe_layer_desc* desc, const void* Xq, const float* Xs,
+                                 const int32_t* offsets, const ec2moe_fp8_weights* w, const float* topk_w,
+                                 const int32_t* perm, void* slot_out, void* workspace, size_t ws_bytes,
+                                 ec2moe_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Balance of the gate. */
+
+/* Bytes of device workspace ec2moe_gate_logits needs (0 on an invalid desc). */
+size_t ec2moe_gate_logits_workspace_size(const ec2moe_layer_desc* desc);
+
+/* The gate's logits to fp32 accuracy: logits[t] = (W_local x_t + b_local,
+ * W_global x_t + b_global), fp32 [T, E + K] (K = n_groups; [T, E] when it is 1).
+ * Passage: Eq. 5 and Eq. 6 before their softmaxes. */
+ec2moe_status ec2moe_gate_logits(const ec2moe_layer_desc* desc, const void* X, const float* W_local,
+                                 const float* b_local, const float* W_global, const float* b_global, float* logits,
+                                 void* workspace, size_t ws_bytes, ec2moe_stream_t stream);
+
+/* Bytes of device workspace ec2moe_balance_loss needs (0 on an invalid desc or n_seg < 1). */
+size_t ec2moe_balance_loss_workspace_size(const ec2moe_layer_desc* desc, int32_t n_seg);
+
+/* Per-expert counts, the balance loss of the gate and its gradients.
+ * With n_s the tokens of segment s that count, c_si the entries of their topk_idx
+ * that name expert i, A the number of allowed experts, S' the number of segments
+ * with n_s > 0 and g the gate's probabilities (Eq. 5-7 under mask and
+ * desc->top_groups):
+ *   f_si = c_si / (k n_s),  P_si = (1 / n_s) sum_t g_i(t),
+ *   loss = coef / S' sum_s A sum_i f_si P_si
+ * (coef when the experts are used evenly; 0 without such a segment).  The counts
+ * are constants of the gradient.  The paper has no counterpart: it is the loss
+ * that trains a gate of Eq. 5-7 towards even loads under a device's mask.
+ *  logits      fp32 [T, E + K] of pitch ld >= E + K (ec2moe_gate_logits); those of
+ *              masked experts and of groups without an allowed one are not used
+ *  mask        host uint8 [E], as for ec2moe_gate
+ *  topk_idx    int32 [T, k] (ec2moe_gate)
+ *  valid       device uint8 [T]: 0 = a token that does not count (padding); NULL:
+ *              all do
+ *  seg_offsets device int32 [n_seg + 1], not decreasing, within [0, T]: segment s
+ *              is the tokens [seg_offsets[s], seg_offsets[s + 1]), possibly none;
+ *              tokens of no segment do not count.  NULL with n_seg = 1: all tokens
+ *  d_loss      device fp32 scalar, the gradient that arrives at the loss (NULL: 1)
+ *  loss        out fp32 scalar
+ *  counts      out int32 [n_seg, E]: c_si
+ *  d_logits    out fp32 [T, E + K] dense, or NULL: d_loss times the gradient; 0 for
+ *              what is masked, pruned or does not count
+ *  d_bias      out fp32 [E + K] or NULL: the gradient in (b_local, b_global), the
+ *              sum of d_logits over the tokens.  The gate rows' gradients are the
+ *              products d_logits^T X, the activations' d_logits (W_local; W_global).
+ * The sums are in a fixed order: the same inputs give the same bits.  An id of
+ * topk_idx outside [0, E) is skipped (not counted) and a segment bound outside
+ * [0, T] or decreasing cuts no token that other bounds do not hold;
+ * ec2moe_last_device_error then reports EC2MOE_ERR_INVALID_ARG.  With T = 0 loss,
+ * counts and d_bias are 0. */
+ec2moe_status ec2moe_balance_loss(const ec2moe_layer_desc* desc, const float* logits, int64_t ld,
+                                  const uint8_t* mask, const int32_t* topk_idx, const uint8_t* valid,
+                                  const int32_t* seg_offsets, int32_t n_seg, float coef, const float* d_loss,
+                                  float* loss, int32_t* counts, float* d_logits, float* d_bias, void* workspace,
+                                  size_t ws_bytes, ec2moe_stream_t stream);
+
 /* Number of kernels the last successful call on this host thread enqueued. */
 int32_t ec2moe_last_launch_count(void);
 
@@ -341,7 +477,9 @@ int32_t ec2moe_last_launch_count(void);
  * ("gate_prep", "gate_topk", "gate_decide", "route_count", "route_scatter", "gather_rows",
  * "lr_encode", "lr_reduce", "lr_decode", "lr_codec", "expert_up", "expert_down", "shared_up",
  * "shared_down", "ffn_up", "ffn_down" (routed and shared experts in one launch),
- * "combine", "sum_counts"); `ms` its device duration.  Profiling is off by default and
+ * "combine", "sum_counts", "quantize_rows", "quantize_blocks", "fp8_gemm", "fp8_up",
+ * "fp8_down", "logits_prep", "logits_gemm", "logits_sum", "balance_clear",
+ * "balance_count", "balance_main", "balance_final"); `ms` its device duration.  Profiling is off by default and
  * costs nothing when off. */
 ec2moe_status ec2moe_profile_enable(int32_t enable);
 /* Restricts profiling to one launch per call: with launch_index >= 0 only the

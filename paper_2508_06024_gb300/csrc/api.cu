@@ -567,6 +567,37 @@ cudaError_t run_expert_stage(const ec2moe_layer_desc* d, const ec2moe_layer_weig
   return cudaSuccess;
 }
 
+// 8-bit products: sizes that the kernels' 32-bit indexes and 16-byte rows take.
+ec2moe_status check_fp8_shape(int n_groups, int rows, int N, int K) {
+  if (n_groups <= 0 || rows < 0 || N <= 0 || K <= 0) return EC2MOE_ERR_INVALID_ARG;
+  if (n_groups > EC2MOE_MAX_EXPERTS) return EC2MOE_ERR_UNSUPPORTED;
+  if (N % 16 != 0 || K % 16 != 0) return EC2MOE_ERR_MISALIGNED;
+  // rows of B, and tiles of C (of 128 x 128 at least, a partial one per group)
+  if ((long long)n_groups * N > 0x7fffffffLL) return EC2MOE_ERR_UNSUPPORTED;
+  if (((long long)rows / 128 + n_groups) * ((N + 127) / 128) > 0x7fffffffLL) return EC2MOE_ERR_UNSUPPORTED;
+  return EC2MOE_OK;
+}
+
+ec2moe_status check_fp8_experts(const ec2moe_layer_desc* d) {
+  ec2moe_status st = check_desc(d);
+  if (st != EC2MOE_OK) return st;
+  const int rows = d->T * d->k;
+  st = check_fp8_shape(d->E, rows, d->d_ff, d->d);
+  return st != EC2MOE_OK ? st : check_fp8_shape(d->E, rows, d->d, d->d_ff);
+}
+
+// Workspace of ec2moe_experts_fp8: hidden rows (at 0), their scales.
+struct Fp8Ws {
+  size_t hs, total;
+};
+Fp8Ws fp8_ws(const ec2moe_layer_desc* d) {
+  const size_t rows = (size_t)d->T * d->k, nb = (d->d_ff + EC2MOE_FP8_BLOCK - 1) / EC2MOE_FP8_BLOCK;
+  Fp8Ws w;
+  w.hs = align_up(rows * d->d_ff);
+  w.total = w.hs + align_up(rows * nb * 4);
+  return w;
+}
+
 // Argument checks of a whole-layer call (everything but the workspace).
 ec2moe_status check_layer_call(const ec2moe_layer_desc* desc, const ec2moe_layer_weights* w, const void* X,
                                const uint8_t* mask, void* Y, int32_t* topk_idx, float* topk_w, int32_t* counts,
@@ -1072,9 +1103,223 @@ ec2moe_status ec2moe_layer_forward_pipelined(const ec2moe_layer_desc* desc, cons
   return EC2MOE_OK;
 }
 
+// ----------------------------------------------------------- 8-bit experts
+ec2moe_status ec2moe_fp8_quantize(int32_t dtype, int32_t n_mats, int32_t rows, int32_t cols, int64_t ld,
+                                  const void* X, int32_t block_rows, const int32_t* inv_perm, int32_t k, void* Q,
+                                  float* scale, ec2moe_stream_t stream) {
+  reset_launch_count();
+  if (dtype != EC2MOE_F32 && dtype != EC2MOE_BF16) return EC2MOE_ERR_INVALID_ARG;
+  if (n_mats < 0 || rows < 0 || cols <= 0 || ld < cols) return EC2MOE_ERR_INVALID_ARG;
+  if (block_rows != 1 && block_rows != EC2MOE_FP8_BLOCK) return EC2MOE_ERR_INVALID_ARG;
+  if (inv_perm ? (block_rows != 1 || n_mats != 1 || k < 1) : k != 0) return EC2MOE_ERR_INVALID_ARG;
+  if (k > EC2MOE_MAX_TOPK) return EC2MOE_ERR_UNSUPPORTED;
+  const int64_t es = dtype == EC2MOE_BF16 ? 2 : 4;
+  if (cols % 16 != 0 || ld * es % 16 != 0) return EC2MOE_ERR_MISALIGNED;
+  const long long n = (long long)n_mats * rows;
+  const long long n_kb = (cols + EC2MOE_FP8_BLOCK - 1) / EC2MOE_FP8_BLOCK;
+  // rows and launch sizes are 32-bit
+  if (n > 0x7fffffffLL || n * (k > 0 ? k : 1) > 0x7fffffffLL || n * n_kb > 0x7fffffffLL) return EC2MOE_ERR_UNSUPPORTED;
+  if (n == 0) return EC2MOE_OK;
+  EC2MOE_REQUIRE_PTR(X);
+  EC2MOE_REQUIRE_PTR(Q);
+  if (!scale) return EC2MOE_ERR_INVALID_ARG;
+  const QuantArgs a{X, ld, n_mats, rows, cols, block_rows, inv_perm, k, Q, scale};
+  EC2MOE_CUDA(launch_quantize(a, dtype == EC2MOE_BF16, stream));
+  return EC2MOE_OK;
+}
+
+size_t ec2moe_fp8_gemm_workspace_size(int32_t n_groups, int32_t rows, int32_t N, int32_t K) {
+  if (check_fp8_shape(n_groups, rows, N, K) != EC2MOE_OK) return 0;
+  return 0;
+}
+
+ec2moe_status ec2moe_fp8_gemm(int32_t n_groups, int32_t rows, int32_t N, int32_t K, const void* A,
+                              const float* A_scale, const int32_t* offsets, const void* B, const float* B_scale,
+                              int32_t out_dtype, void* C, int64_t ldc, void* workspace, size_t ws_bytes,
+                              ec2moe_stream_t stream) {
+  reset_launch_count();
+  ec2moe_status st = check_fp8_shape(n_groups, rows, N, K);
+  if (st != EC2MOE_OK) return st;
+  if (out_dtype != EC2MOE_F32 && out_dtype != EC2MOE_BF16) return EC2MOE_ERR_INVALID_ARG;
+  if (ldc < N || (!offsets && n_groups != 1)) return EC2MOE_ERR_INVALID_ARG;
+  if (ldc * (out_dtype == EC2MOE_BF16 ? 2 : 4) % 16 != 0) return EC2MOE_ERR_MISALIGNED;
+  if (rows == 0) return EC2MOE_OK;
+  EC2MOE_REQUIRE_PTR(A);
+  EC2MOE_REQUIRE_PTR(B);
+  EC2MOE_REQUIRE_PTR(C);
+  if (!A_scale || !B_scale) return EC2MOE_ERR_INVALID_ARG;
+  (void)workspace;
+  (void)ws_bytes;
+  Fp8GemmArgs g{};
+  g.timeout_cycles = default_timeout_cycles();
+  g.name = "fp8_gemm";
+  g.A = A;
+  g.SA = A_scale;
+  g.B = B;
+  g.SB = B_scale;
+  g.offsets = offsets;
+  g.G = n_groups;
+  g.rows = rows;
+  g.N = N;
+  g.K = K;
+  g.out = C;
+  g.ldo = ldc;
+  g.out_bf16 = out_dtype == EC2MOE_BF16;
+  EC2MOE_CUDA(launch_gemm_fp8(g, EPI_STORE, stream));
+  return EC2MOE_OK;
+}
+
+size_t ec2moe_experts_fp8_workspace_size(const ec2moe_layer_desc* desc) {
+  if (check_fp8_experts(desc) != EC2MOE_OK) return 0;
+  return fp8_ws(desc).total;
+}
+
+ec2moe_status ec2moe_experts_fp8(const ec2moe_layer_desc* desc, const void* Xq, const float* Xs,
+                                 const int32_t* offsets, const ec2moe_fp8_weights* w, const float* topk_w,
+                                 const int32_t* perm, void* slot_out, void* workspace, size_t ws_bytes,
+                                 ec2moe_stream_t stream) {
+  reset_launch_count();
+  ec2moe_status st = check_fp8_experts(desc);
+  if (st != EC2MOE_OK) return st;
+  if (!w) return EC2MOE_ERR_INVALID_ARG;
+  if (desc->T == 0) return EC2MOE_OK;
+  const bool glu = desc->act == EC2MOE_SWIGLU;
+  EC2MOE_REQUIRE_PTR(Xq);
+  EC2MOE_REQUIRE_PTR(w->W1);
+  EC2MOE_REQUIRE_PTR(w->W2);
+  if (glu) EC2MOE_REQUIRE_PTR(w->W3);
+  EC2MOE_REQUIRE_PTR(slot_out);
+  if (!Xs || !w->S1 || !w->S2 || (glu && !w->S3) || !offsets || !topk_w || !perm) return EC2MOE_ERR_INVALID_ARG;
+  const Fp8Ws L = fp8_ws(desc);
+  if (!workspace || ws_bytes < L.total) return EC2MOE_ERR_WORKSPACE;
+  if (!aligned16(workspace)) return EC2MOE_ERR_MISALIGNED;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  Fp8GemmArgs g{};
+  g.timeout_cycles = default_timeout_cycles();
+  g.name = "fp8_up";
+  g.A = Xq;
+  g.SA = Xs;
+  g.B = w->W1;
+  g.SB = w->S1;
+  g.B2 = w->W3;
+  g.SB2 = w->S3;
+  g.offsets = offsets;
+  g.G = desc->E;
+  g.rows = desc->T * desc->k;
+  g.N = desc->d_ff;
+  g.K = desc->d;
+  g.out = ws;
+  g.out_scale = reinterpret_cast<float*>(ws + L.hs);
+  EC2MOE_CUDA(launch_gemm_fp8(g, glu ? EPI_SWIGLU : EPI_GELU, stream));
+  g.name = "fp8_down";
+  g.A = ws;
+  g.SA = g.out_scale;
+  g.B = w->W2;
+  g.SB = w->S2;
+  g.B2 = nullptr;
+  g.SB2 = nullptr;
+  g.N = desc->d;
+  g.K = desc->d_ff;
+  g.out = slot_out;
+  g.ldo = desc->d;
+  g.out_bf16 = is_bf16(desc);
+  g.out_scale = nullptr;
+  g.perm = perm;
+  g.row_scale = topk_w;
+  EC2MOE_CUDA(launch_gemm_fp8(g, EPI_STORE, stream));
+  return EC2MOE_OK;
+}
+
+// ----------------------------------------------------------- gate logits, balance
+size_t ec2moe_gate_logits_workspace_size(const ec2moe_layer_desc* desc) {
+  if (check_desc(desc) != EC2MOE_OK) return 0;
+  return gate_logits_bytes(desc->T, desc->d, desc->E, desc->n_groups, is_bf16(desc));
+}
+
+ec2moe_status ec2moe_gate_logits(const ec2moe_layer_desc* desc, const void* X, const float* W_local,
+                                 const float* b_local, const float* W_global, const float* b_global, float* logits,
+                                 void* workspace, size_t ws_bytes, ec2moe_stream_t stream) {
+  reset_launch_count();
+  ec2moe_status st = check_desc(desc);
+  if (st != EC2MOE_OK) return st;
+  if (desc->T == 0) return EC2MOE_OK;
+  EC2MOE_REQUIRE_PTR(X);
+  EC2MOE_REQUIRE_PTR(W_local);
+  EC2MOE_REQUIRE_PTR(b_local);
+  if (desc->n_groups > 1) {
+    EC2MOE_REQUIRE_PTR(W_global);
+    EC2MOE_REQUIRE_PTR(b_global);
+  }
+  EC2MOE_REQUIRE_PTR(logits);
+  if (!workspace || ws_bytes < ec2moe_gate_logits_workspace_size(desc)) return EC2MOE_ERR_WORKSPACE;
+  if (!aligned16(workspace)) return EC2MOE_ERR_MISALIGNED;
+  LogitsArgs a{};
+  a.X = X;
+  a.W_local = W_local;
+  a.b_local = b_local;
+  a.W_global = desc->n_groups > 1 ? W_global : nullptr;
+  a.b_global = desc->n_groups > 1 ? b_global : nullptr;
+  a.T = desc->T;
+  a.d = desc->d;
+  a.E = desc->E;
+  a.K = desc->n_groups;
+  a.logits = logits;
+  a.workspace = workspace;
+  a.timeout_cycles = default_timeout_cycles();
+  EC2MOE_CUDA(launch_gate_logits(a, is_bf16(desc), stream));
+  return EC2MOE_OK;
+}
+
+size_t ec2moe_balance_loss_workspace_size(const ec2moe_layer_desc* desc, int32_t n_seg) {
+  if (check_desc(desc) != EC2MOE_OK || n_seg < 1) return 0;
+  return balance_bytes(desc->T, desc->E, desc->n_groups, n_seg);
+}
+
+ec2moe_status ec2moe_balance_loss(const ec2moe_layer_desc* desc, const float* logits, int64_t ld,
+                                  const uint8_t* mask, const int32_t* topk_idx, const uint8_t* valid,
+                                  const int32_t* seg_offsets, int32_t n_seg, float coef, const float* d_loss,
+                                  float* loss, int32_t* counts, float* d_logits, float* d_bias, void* workspace,
+                                  size_t ws_bytes, ec2moe_stream_t stream) {
+  reset_launch_count();
+  ec2moe_status st = check_desc(desc);
+  if (st != EC2MOE_OK) return st;
+  BalanceArgs a{};
+  st = check_mask(desc, mask, a.mask_bits);
+  if (st != EC2MOE_OK) return st;
+  const int O = desc->E + (desc->n_groups > 1 ? desc->n_groups : 0);
+  if (n_seg < 1 || (!seg_offsets && n_seg != 1) || ld < O) return EC2MOE_ERR_INVALID_ARG;
+  if ((long long)n_seg * desc->E > 0x7fffffffLL) return EC2MOE_ERR_UNSUPPORTED;
+  if (!loss || !counts) return EC2MOE_ERR_INVALID_ARG;
+  if (desc->T > 0 && (!logits || !topk_idx)) return EC2MOE_ERR_INVALID_ARG;
+  if (!workspace || ws_bytes < ec2moe_balance_loss_workspace_size(desc, n_seg)) return EC2MOE_ERR_WORKSPACE;
+  if (!aligned16(workspace)) return EC2MOE_ERR_MISALIGNED;
+  a.logits = logits;
+  a.ld = ld;
+  a.T = desc->T;
+  a.E = desc->E;
+  a.K = desc->n_groups;
+  a.k = desc->k;
+  a.top_groups = desc->top_groups;
+  for (int e = 0; e < desc->E; ++e) a.n_allowed += mask[e] ? 1 : 0;
+  a.topk_idx = topk_idx;
+  a.valid = valid;
+  a.seg_offsets = seg_offsets;
+  a.n_seg = n_seg;
+  a.coef = coef;
+  a.d_loss = d_loss;
+  a.loss = loss;
+  a.counts = counts;
+  a.d_logits = d_logits;
+  a.d_bias = d_bias;
+  a.workspace = workspace;
+  EC2MOE_CUDA(launch_balance(a, stream));
+  return EC2MOE_OK;
+}
+
 ec2moe_status ec2moe_last_device_error(ec2moe_stream_t stream) {
   if (cudaStreamSynchronize(stream) != cudaSuccess) return EC2MOE_ERR_CUDA;
-  unsigned int tc = 0, codec = 0, gate = 0, route = 0, swap = 0, skinny = 0, f32 = 0, tok = 0;
+  unsigned int tc = 0, codec = 0, gate = 0, route = 0, swap = 0, skinny = 0, f32 = 0, tok = 0, fp8 = 0, quant = 0,
+               balance = 0;
   if (read_tc_error(&tc) != cudaSuccess) return EC2MOE_ERR_CUDA;
   if (read_codec_error(&codec) != cudaSuccess) return EC2MOE_ERR_CUDA;
   if (read_gate_error(&gate) != cudaSuccess) return EC2MOE_ERR_CUDA;
@@ -1083,11 +1328,14 @@ ec2moe_status ec2moe_last_device_error(ec2moe_stream_t stream) {
   if (read_skinny_error(&skinny) != cudaSuccess) return EC2MOE_ERR_CUDA;
   if (read_f32_error(&f32) != cudaSuccess) return EC2MOE_ERR_CUDA;
   if (read_tok_error(&tok) != cudaSuccess) return EC2MOE_ERR_CUDA;
+  if (read_fp8_error(&fp8) != cudaSuccess) return EC2MOE_ERR_CUDA;
+  if (read_quant_error(&quant) != cudaSuccess) return EC2MOE_ERR_CUDA;
+  if (read_balance_error(&balance) != cudaSuccess) return EC2MOE_ERR_CUDA;
   // bit 0 of the GEMM, codec and gate words: a bounded wait timed out;
-  // bit 1 of the GEMM words and any bit of the routing word: an index outside
-  // the call's rows or experts was skipped
-  if ((tc | codec | gate | swap | f32 | tok) & 1u) return EC2MOE_ERR_TIMEOUT;
-  if (((tc | swap | skinny | f32 | tok) & 2u) || route) return EC2MOE_ERR_INVALID_ARG;
+  // bit 1 of the GEMM words and any bit of the routing, quantiser and balance
+  // words: an index outside the call's rows or experts was skipped
+  if ((tc | codec | gate | swap | f32 | tok | fp8) & 1u) return EC2MOE_ERR_TIMEOUT;
+  if (((tc | swap | skinny | f32 | tok | fp8) & 2u) || route || quant || balance) return EC2MOE_ERR_INVALID_ARG;
   return EC2MOE_OK;
 }
 

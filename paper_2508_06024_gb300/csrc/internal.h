@@ -262,6 +262,94 @@ cudaError_t read_swap_error(unsigned int* word);
 bool make_tensor_map_bf16(CUtensorMap* m, const void* ptr, long long rows, long long cols, int box_rows);
 // 2-D fp32 tensor map, box 64 columns x box_rows rows, no swizzle (cached).
 bool make_tensor_map_f32(CUtensorMap* m, const void* ptr, long long rows, long long cols, int box_rows);
+// 2-D tensor map over bytes, box 128 columns x box_rows rows, 128-byte swizzle,
+// zero fill out of bounds (cached).
+bool make_tensor_map_u8(CUtensorMap* m, const void* ptr, long long rows, long long cols, int box_rows);
+
+// ------------------------------------------------------------------ 8-bit path
+// X [n_mats * rows, cols] (pitch ld elements) to e4m3 with a scale per block of
+// 128 columns of a row (block_rows 1) or of 128 rows of a matrix (128).
+// inv_perm (block_rows 1): row t goes to the rows inv_perm[t * k + s], s < k.
+struct QuantArgs {
+  const void* X;
+  long long ld;
+  int n_mats, rows, cols, block_rows;
+  const int32_t* inv_perm;
+  int k;
+  void* Q;
+  float* scale;
+};
+cudaError_t launch_quantize(const QuantArgs& a, bool bf16, cudaStream_t s);
+// Reads and clears the quantiser's device error word (synchronous): nonzero
+// when a placement outside the call's rows was skipped.
+cudaError_t read_quant_error(unsigned int* word);
+
+// C_g = A_g B_g^T over e4m3 rows with 1 x 128 scales and weights with 128 x 128
+// scales; group g owns rows [offsets[g], offsets[g+1]) of A (offsets == nullptr:
+// one group of all rows).  EPI_STORE writes bf16 or fp32, to row perm[row] times
+// row_scale[perm[row]] where those are given; EPI_GELU and EPI_SWIGLU write the
+// activation's result quantised again, rows of N bytes and ceil(N / 128) scales.
+struct Fp8GemmArgs {
+  const void* A;
+  const float* SA;
+  const void* B;
+  const float* SB;
+  const void* B2;       // SwiGLU: W3
+  const float* SB2;
+  const int32_t* offsets;
+  int G, rows, N, K;
+  void* out;
+  long long ldo;        // EPI_STORE: pitch in elements
+  bool out_bf16;
+  float* out_scale;
+  const int32_t* perm;
+  const float* row_scale;
+  int g_active;         // groups expected to hold rows (0 = G)
+  long long timeout_cycles;
+  const char* name;
+};
+cudaError_t launch_gemm_fp8(const Fp8GemmArgs& a, int epi, cudaStream_t s);
+// Reads and clears the 8-bit GEMM's device error word (bits as read_tc_error).
+cudaError_t read_fp8_error(unsigned int* word);
+
+// ------------------------------------------------------- gate logits and balance
+struct LogitsArgs {
+  const void* X;
+  const float* W_local;
+  const float* b_local;
+  const float* W_global;  // nullptr when K == 1
+  const float* b_global;
+  int T, d, E, K;
+  float* logits;          // [T, E + K], K = 0 rows without a global gate
+  void* workspace;
+  long long timeout_cycles;
+};
+size_t gate_logits_bytes(int T, int d, int E, int K, bool bf16);
+cudaError_t launch_gate_logits(const LogitsArgs& a, bool bf16, cudaStream_t s);
+
+struct BalanceArgs {
+  const float* logits;        // pitch ld
+  long long ld;
+  uint32_t mask_bits[4];
+  int T, E, K, k, top_groups;
+  int n_allowed;
+  const int32_t* topk_idx;
+  const uint8_t* valid;       // nullptr: every token counts
+  const int32_t* seg_offsets; // nullptr: one segment of all tokens
+  int n_seg;
+  float coef;
+  const float* d_loss;        // nullptr: 1
+  float* loss;
+  int32_t* counts;            // [n_seg, E]
+  float* d_logits;            // [T, E + K] or nullptr
+  float* d_bias;              // [E + K] or nullptr
+  void* workspace;
+};
+size_t balance_bytes(int T, int E, int K, int n_seg);
+cudaError_t launch_balance(const BalanceArgs& a, cudaStream_t s);
+// Reads and clears the balance kernels' device error word (synchronous):
+// nonzero when an expert id or a segment bound out of range was skipped.
+cudaError_t read_balance_error(unsigned int* word);
 
 // Fused low-rank codec of the layer path (bf16): Z = X V_enc^T (stored), then
 // X_hat = Z V_dec^T written straight into expert order with relative

@@ -703,9 +703,9 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   return fn;
 }
 
-// Map kinds: bf16 with the 128-byte swizzle, or fp32 unswizzled (rows of
-// 64 x 4 = 256 bytes in shared memory).
-enum MapKind { MAP_BF16_SW128 = 0, MAP_F32_PLAIN = 1 };
+// Map kinds: bf16 or bytes with the 128-byte swizzle (64 or 128 columns), or
+// fp32 unswizzled (rows of 64 x 4 = 256 bytes in shared memory).
+enum MapKind { MAP_BF16_SW128 = 0, MAP_F32_PLAIN = 1, MAP_U8_SW128 = 2 };
 
 bool encode_map(CUtensorMap* m, const void* ptr, long long rows, long long cols, int box_rows, int kind);
 
@@ -725,8 +725,8 @@ struct MapKey {
   }
 };
 
-// 2-D tensor map over a row-major [rows, cols] matrix, box = 64 columns x
-// box_rows rows, zero fill out of bounds.
+// 2-D tensor map over a row-major [rows, cols] matrix, box = 64 columns (128 of
+// bytes) x box_rows rows, zero fill out of bounds.
 bool make_map(CUtensorMap* m, const void* ptr, long long rows, long long cols, int box_rows,
               int kind = MAP_BF16_SW128) {
   constexpr int SLOTS = 64;
@@ -758,13 +758,13 @@ bool make_map(CUtensorMap* m, const void* ptr, long long rows, long long cols, i
 bool encode_map(CUtensorMap* m, const void* ptr, long long rows, long long cols, int box_rows, int kind) {
   auto fn = encode_fn();
   if (!fn) return false;
-  const bool f32 = kind == MAP_F32_PLAIN;
+  const bool f32 = kind == MAP_F32_PLAIN, u8 = kind == MAP_U8_SW128;
   cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
-  cuuint64_t strides[1] = {static_cast<cuuint64_t>(cols) * (f32 ? 4 : 2)};
-  cuuint32_t box[2] = {static_cast<cuuint32_t>(BK), static_cast<cuuint32_t>(box_rows)};
+  cuuint64_t strides[1] = {static_cast<cuuint64_t>(cols) * (f32 ? 4 : u8 ? 1 : 2)};
+  cuuint32_t box[2] = {static_cast<cuuint32_t>(u8 ? 2 * BK : BK), static_cast<cuuint32_t>(box_rows)};
   cuuint32_t estr[2] = {1, 1};
-  CUresult r = fn(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2,
-                  const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  CUresult r = fn(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : u8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+                  2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   f32 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS;
@@ -966,6 +966,10 @@ bool make_tensor_map_bf16(CUtensorMap* m, const void* ptr, long long rows, long 
 
 bool make_tensor_map_f32(CUtensorMap* m, const void* ptr, long long rows, long long cols, int box_rows) {
   return make_map(m, ptr, rows, cols, box_rows, MAP_F32_PLAIN);
+}
+
+bool make_tensor_map_u8(CUtensorMap* m, const void* ptr, long long rows, long long cols, int box_rows) {
+  return make_map(m, ptr, rows, cols, box_rows, MAP_U8_SW128);
 }
 
 // Whether a grouped GEMM runs on CTA pairs (256-row tiles): for the row-

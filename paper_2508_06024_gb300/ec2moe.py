@@ -42,7 +42,12 @@ EXPORTED = [
     "ec2moe_profile_read", "ec2moe_profile_reset", "ec2moe_route_noalloc", "ec2moe_set_wait_budget",
     "ec2moe_get_wait_budget", "ec2moe_schedule", "ec2moe_schedule_objective", "ec2moe_expert_tasks",
     "ec2moe_pipelined_workspace_size", "ec2moe_layer_forward_pipelined", "ec2moe_profile_only",
+    "ec2moe_fp8_quantize", "ec2moe_fp8_gemm_workspace_size", "ec2moe_fp8_gemm", "ec2moe_experts_fp8_workspace_size",
+    "ec2moe_experts_fp8", "ec2moe_gate_logits_workspace_size", "ec2moe_gate_logits",
+    "ec2moe_balance_loss_workspace_size", "ec2moe_balance_loss",
 ]
+
+FP8_BLOCK = 128  # columns (and weight rows) that share a scale
 
 END = 0
 CLOUD = 1
@@ -58,6 +63,10 @@ class LayerWeights(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in
                 ("W_local", "b_local", "W_global", "b_global", "W1", "W3", "W2", "W1s", "W3s", "W2s",
                  "V_enc", "V_dec")]
+
+
+class Fp8Weights(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("W1", "S1", "W3", "S3", "W2", "S2")]
 
 
 class Ec2moeError(RuntimeError):
@@ -103,6 +112,19 @@ _SIGS = {
     "ec2moe_pipelined_workspace_size": (ctypes.c_size_t, [_D, ctypes.c_int32]),
     "ec2moe_layer_forward_pipelined": (ctypes.c_int, [_D, ctypes.POINTER(LayerWeights), _P, _P, _P, _P, _P, _P, _P,
                                                       _P, ctypes.c_size_t, ctypes.c_int32, _P, _P]),
+    "ec2moe_fp8_quantize": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                                           ctypes.c_int64, _P, ctypes.c_int32, _P, ctypes.c_int32, _P, _P, _P]),
+    "ec2moe_fp8_gemm_workspace_size": (ctypes.c_size_t, [ctypes.c_int32] * 4),
+    "ec2moe_fp8_gemm": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _P, _P, _P, _P,
+                                       _P, ctypes.c_int32, _P, ctypes.c_int64, _P, ctypes.c_size_t, _P]),
+    "ec2moe_experts_fp8_workspace_size": (ctypes.c_size_t, [_D]),
+    "ec2moe_experts_fp8": (ctypes.c_int, [_D, _P, _P, _P, ctypes.POINTER(Fp8Weights), _P, _P, _P, _P, ctypes.c_size_t,
+                                          _P]),
+    "ec2moe_gate_logits_workspace_size": (ctypes.c_size_t, [_D]),
+    "ec2moe_gate_logits": (ctypes.c_int, [_D, _P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
+    "ec2moe_balance_loss_workspace_size": (ctypes.c_size_t, [_D, ctypes.c_int32]),
+    "ec2moe_balance_loss": (ctypes.c_int, [_D, _P, ctypes.c_int64, _P, _P, _P, _P, ctypes.c_int32, ctypes.c_float, _P,
+                                           _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
 }
 
 
@@ -173,6 +195,10 @@ def make_weights(W_local=None, b_local=None, W_global=None, b_global=None, W1=No
                  W1s=None, W3s=None, W2s=None, V_enc=None, V_dec=None) -> LayerWeights:
     return LayerWeights(*(_ptr(t) for t in (W_local, b_local, W_global, b_global, W1, W3, W2, W1s, W3s, W2s,
                                             V_enc, V_dec)))
+
+
+def make_fp8_weights(W1=None, S1=None, W3=None, S3=None, W2=None, S2=None) -> Fp8Weights:
+    return Fp8Weights(*(_ptr(t) for t in (W1, S1, W3, S3, W2, S2)))
 
 
 def ec2moe_workspace_size(desc: LayerDesc) -> int:
@@ -293,6 +319,63 @@ def ec2moe_set_wait_budget(cycles: int) -> None:
 
 def ec2moe_get_wait_budget() -> int:
     return int(load().ec2moe_get_wait_budget())
+
+
+# ----------------------------------------------------------------- 8-bit experts
+def ec2moe_fp8_quantize(dtype, n_mats, rows, cols, ld, X, block_rows, inv_perm, k, Q, scale, stream=None):
+    """X [n_mats * rows, cols] (pitch ld) to e4m3 with a scale per block of 1 or 128 rows x 128 columns."""
+    _check(load().ec2moe_fp8_quantize(int(dtype), int(n_mats), int(rows), int(cols), int(ld), _ptr(X), int(block_rows),
+                                      _ptr(inv_perm), int(k), _ptr(Q), _ptr(scale), _stream(stream)),
+           "ec2moe_fp8_quantize")
+
+
+def ec2moe_fp8_gemm_workspace_size(n_groups: int, rows: int, N: int, K: int) -> int:
+    return int(load().ec2moe_fp8_gemm_workspace_size(int(n_groups), int(rows), int(N), int(K)))
+
+
+def ec2moe_fp8_gemm(n_groups, rows, N, K, A, A_scale, offsets, B, B_scale, out_dtype, out, ldc, workspace=None,
+                    ws_bytes=0, stream=None):
+    """out_g = A_g B_g^T over the groups of rows that `offsets` names (None: one group)."""
+    _check(load().ec2moe_fp8_gemm(int(n_groups), int(rows), int(N), int(K), _ptr(A), _ptr(A_scale), _ptr(offsets),
+                                  _ptr(B), _ptr(B_scale), int(out_dtype), _ptr(out), int(ldc), _ptr(workspace),
+                                  int(ws_bytes), _stream(stream)), "ec2moe_fp8_gemm")
+
+
+def ec2moe_experts_fp8_workspace_size(desc: LayerDesc) -> int:
+    return int(load().ec2moe_experts_fp8_workspace_size(_dref(desc)))
+
+
+def ec2moe_experts_fp8(desc, Xq, Xs, offsets, weights: Fp8Weights, topk_w, perm, slot_out, workspace, ws_bytes,
+                       stream=None):
+    _check(load().ec2moe_experts_fp8(_dref(desc), _ptr(Xq), _ptr(Xs), _ptr(offsets),
+                                     None if weights is None else ctypes.byref(weights), _ptr(topk_w), _ptr(perm),
+                                     _ptr(slot_out), _ptr(workspace), int(ws_bytes), _stream(stream)),
+           "ec2moe_experts_fp8")
+
+
+# ----------------------------------------------------------------- balance of the gate
+def ec2moe_gate_logits_workspace_size(desc: LayerDesc) -> int:
+    return int(load().ec2moe_gate_logits_workspace_size(_dref(desc)))
+
+
+def ec2moe_gate_logits(desc, X, W_local, b_local, W_global, b_global, logits, workspace, ws_bytes, stream=None):
+    """logits [T, E + K] in fp32 accuracy (K = 0 columns when n_groups is 1)."""
+    _check(load().ec2moe_gate_logits(_dref(desc), _ptr(X), _ptr(W_local), _ptr(b_local), _ptr(W_global),
+                                     _ptr(b_global), _ptr(logits), _ptr(workspace), int(ws_bytes), _stream(stream)),
+           "ec2moe_gate_logits")
+
+
+def ec2moe_balance_loss_workspace_size(desc: LayerDesc, n_seg: int) -> int:
+    return int(load().ec2moe_balance_loss_workspace_size(_dref(desc), int(n_seg)))
+
+
+def ec2moe_balance_loss(desc, logits, ld, mask, topk_idx, valid, seg_offsets, n_seg, coef, d_loss, loss, counts,
+                        d_logits, d_bias, workspace, ws_bytes, stream=None):
+    """Counts per segment and expert, the balance loss and its gradients in the logits and the biases."""
+    _check(load().ec2moe_balance_loss(_dref(desc), _ptr(logits), int(ld), _mask(mask), _ptr(topk_idx), _ptr(valid),
+                                      _ptr(seg_offsets), int(n_seg), float(coef), _ptr(d_loss), _ptr(loss),
+                                      _ptr(counts), _ptr(d_logits), _ptr(d_bias), _ptr(workspace), int(ws_bytes),
+                                      _stream(stream)), "ec2moe_balance_loss")
 
 
 # ----------------------------------------------------------------- scheduler (host)
