@@ -586,15 +586,18 @@ ec2moe_status check_fp8_experts(const ec2moe_layer_desc* d) {
   return st != EC2MOE_OK ? st : check_fp8_shape(d->E, rows, d->d, d->d_ff);
 }
 
-// Workspace of ec2moe_experts_fp8: hidden rows (at 0), their scales.
+// Workspace of ec2moe_experts_fp8: hidden rows (at 0), their scales (a row's
+// padded to 16 bytes, so that the down projection copies four at once).
 struct Fp8Ws {
   size_t hs, total;
+  int hs_pitch;
 };
 Fp8Ws fp8_ws(const ec2moe_layer_desc* d) {
-  const size_t rows = (size_t)d->T * d->k, nb = (d->d_ff + EC2MOE_FP8_BLOCK - 1) / EC2MOE_FP8_BLOCK;
+  const size_t rows = (size_t)d->T * d->k;
   Fp8Ws w;
+  w.hs_pitch = ((d->d_ff + EC2MOE_FP8_BLOCK - 1) / EC2MOE_FP8_BLOCK + 3) / 4 * 4;
   w.hs = align_up(rows * d->d_ff);
-  w.total = w.hs + align_up(rows * nb * 4);
+  w.total = w.hs + align_up(rows * w.hs_pitch * 4);
   return w;
 }
 
@@ -1210,10 +1213,12 @@ ec2moe_status ec2moe_experts_fp8(const ec2moe_layer_desc* desc, const void* Xq, 
   g.K = desc->d;
   g.out = ws;
   g.out_scale = reinterpret_cast<float*>(ws + L.hs);
+  g.out_scale_pitch = L.hs_pitch;
   EC2MOE_CUDA(launch_gemm_fp8(g, glu ? EPI_SWIGLU : EPI_GELU, stream));
   g.name = "fp8_down";
   g.A = ws;
   g.SA = g.out_scale;
+  g.sa_pitch = L.hs_pitch;
   g.B = w->W2;
   g.SB = w->S2;
   g.B2 = nullptr;

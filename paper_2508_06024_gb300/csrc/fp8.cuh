@@ -35,44 +35,40 @@ __device__ __forceinline__ U4 fp8_pack16(const float* v, float inv) {
   return U4{w[0], w[1], w[2], w[3]};
 }
 
-// Packed pairs of fp32 (one instruction for two multiply-adds).
-__device__ __forceinline__ uint64_t f32x2(float lo, float hi) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ uint64_t f32x2_bits(uint32_t lo, uint32_t hi) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
-  return r;
-}
-__device__ __forceinline__ float2 f32x2_get(uint64_t v) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-  return r;
-}
-__device__ __forceinline__ uint64_t f32x2_fma(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ uint64_t f32x2_mul(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-
 namespace tc {
 
-// tcgen05.wait::ld, with the 16 registers that the loads fill as operands, so
-// that nothing which reads them is moved before it.
-__device__ __forceinline__ void tmem_wait_for16(uint32_t* r) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
-                 "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
-               :
-               : "memory");
+// 32 lanes x 64 columns of fp32 TMEM words: thread i of the warp receives columns
+// [col, col + 64) of TMEM lane (quadrant base + i).  Loads and wait are one
+// statement, so nothing that reads the values is moved before the wait.
+__device__ __forceinline__ void tmem_ld64(uint32_t taddr, float* v) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%64];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
+      "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%65];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=&f"(v[0]), "=&f"(v[1]), "=&f"(v[2]), "=&f"(v[3]), "=&f"(v[4]), "=&f"(v[5]), "=&f"(v[6]), "=&f"(v[7]),
+        "=&f"(v[8]), "=&f"(v[9]), "=&f"(v[10]), "=&f"(v[11]), "=&f"(v[12]), "=&f"(v[13]), "=&f"(v[14]), "=&f"(v[15]),
+        "=&f"(v[16]), "=&f"(v[17]), "=&f"(v[18]), "=&f"(v[19]), "=&f"(v[20]), "=&f"(v[21]), "=&f"(v[22]), "=&f"(v[23]),
+        "=&f"(v[24]), "=&f"(v[25]), "=&f"(v[26]), "=&f"(v[27]), "=&f"(v[28]), "=&f"(v[29]), "=&f"(v[30]), "=&f"(v[31]),
+        "=&f"(v[32]), "=&f"(v[33]), "=&f"(v[34]), "=&f"(v[35]), "=&f"(v[36]), "=&f"(v[37]), "=&f"(v[38]), "=&f"(v[39]),
+        "=&f"(v[40]), "=&f"(v[41]), "=&f"(v[42]), "=&f"(v[43]), "=&f"(v[44]), "=&f"(v[45]), "=&f"(v[46]), "=&f"(v[47]),
+        "=&f"(v[48]), "=&f"(v[49]), "=&f"(v[50]), "=&f"(v[51]), "=&f"(v[52]), "=&f"(v[53]), "=&f"(v[54]), "=&f"(v[55]),
+        "=&f"(v[56]), "=&f"(v[57]), "=&f"(v[58]), "=&f"(v[59]), "=&f"(v[60]), "=&f"(v[61]), "=&f"(v[62]), "=&f"(v[63])
+      : "r"(taddr), "r"(taddr + 32)
+      : "memory");
 }
+
+// Asynchronous copy of 4, 8 or 16 bytes to shared memory; cp_async_arrive counts
+// one arrival on the barrier once the calling thread's copies so far have landed.
+template <int BYTES>
+__device__ __forceinline__ void cp_async(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // Instruction descriptor of tcgen05.mma kind::f8f6f4: fp32 accumulator (bits 4-5
 // = 1), A and B e4m3 (bits 7-9 and 10-12 = 0), both K-major, N >> 3 in bits

@@ -8,15 +8,17 @@
 // and its four MMAs leave the block's unscaled sums in tensor memory.  The scales
 // are arbitrary fp32 numbers, so every block's sums leave tensor memory: eight
 // warps read them and multiply-add them into fp32 registers with the row's scale
-// (a thread's TMEM lane is its row) times the column block's, two per
-// instruction, while the MMAs fill the other of two tensor-memory buffers.
+// (a thread's TMEM lane is its row) times the column block's, while the MMAs fill
+// the other of two tensor-memory buffers.
 //
-// CTA layout (320 threads):
-//   warp 0      TMA producer
-//   warp 1      TMEM allocator and MMA issuer
-//   warps 2..9  sums: warp w reads TMEM lanes 32 (w % 4) .. +31, and of the
-//               tile's two halves of 128 columns the 64 of each that (w - 2) / 4
-//               names; at the end of a tile its epilogue.
+// CTA layout (384 threads):
+//   warp 0       TMA producer
+//   warp 1       TMEM allocator and MMA issuer
+//   warp 2       scales: the rows' and the column blocks' of each block of K, from
+//                global memory to a ring in shared memory
+//   warps 4..11  sums: warp w reads TMEM lanes 32 (w % 4) .. +31, and of the
+//                tile's two halves of 128 columns the 64 of each that (w - 4) / 4
+//                names; at the end of a tile its epilogue.
 // The two halves are two column blocks of B, or (SwiGLU) the same block of W1
 // and W3, so that a thread holds both factors of its hidden values.  Their
 // result is quantised here, from the fp32 values: the two warps that hold a
@@ -54,16 +56,27 @@ constexpr int HALF = 128;
 constexpr int BK = FP8_BLOCK;
 constexpr int UK = 32;    // K of one tcgen05.mma kind::f8f6f4
 constexpr int SUM_WARPS = 8;
-constexpr int NUM_THREADS = 64 + 32 * SUM_WARPS;
+constexpr int FIRST_SUM = 4;      // the first warpgroup loads, issues and idles
+constexpr int NUM_THREADS = 32 * (FIRST_SUM + SUM_WARPS);
+// Registers: 384 threads start with 168 each (64512); the sums' warpgroups take
+// what the first one gives up (128 * 56 + 256 * 224 = 64512).
+constexpr int REGS_FEW = 56, REGS_SUM = 224;
 constexpr int MAX_GROUPS = 136;
-constexpr int TMEM_COLS = 2 * BN;
+constexpr int TMEM_COLS = 512;
+// Scales are handed over for SG blocks of K at a time: a wait and a release cost
+// about 200 clocks, a block's MMAs 512.
+constexpr int SG = 4;
+constexpr int RING = 3;              // such groups held
+constexpr int RING_GROUP = (BM + 2) * SG;  // floats: [BM rows][SG], then [SG][2 halves]
 
 // What happens to a tile: stored (bf16 or fp32, optionally scattered and scaled
 // by row), or put through the activation and quantised.
 enum Mode { STORE_BF16 = 0, STORE_F32 = 1, QUANT_GELU = 2, QUANT_SWIGLU = 3 };
 
 struct Params {
-  const float* SA;           // [rows, n_kb]
+  const float* SA;           // [rows, n_kb], pitch sa_pitch
+  int sa_pitch;
+  int sa_words;              // scales per copy: what the pitch and the address align to
   const float* SB;           // [G, n_nb, n_kb]
   const float* SB2;          // SwiGLU: of W3
   const int32_t* offsets;    // [G + 1], nullptr: one group of all rows
@@ -71,7 +84,8 @@ struct Params {
   int n_tiles_n;
   void* out;                 // STORE: [rows, ldo]; QUANT: e4m3 [rows, N]
   long long ldo;
-  float* out_scale;          // QUANT: [rows, ceil(N / 128)]
+  float* out_scale;          // QUANT: [rows, ceil(N / 128)], pitch out_scale_pitch
+  int out_scale_pitch;
   const int32_t* perm;       // STORE: destination of each row (nullptr: itself)
   const float* row_scale;    // STORE: factor of each destination (nullptr: 1)
   long long timeout;
@@ -97,19 +111,23 @@ struct Cfg {
   static constexpr int A_BYTES = BM * BK;
   static constexpr int B_BYTES = B_ROWS * BK;
   static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
-  static constexpr int STAGES = PAIR ? 6 : 4;
+  static constexpr int STAGES = PAIR ? 5 : 4;
   static constexpr int OUT_COLS = MODE == QUANT_SWIGLU ? HALF : BN;  // columns of the result per tile
-  static constexpr int N_BARS = 2 * STAGES + 5;  // full, empty, tfull[2], tempty[2], drain
+  static constexpr int BUFS = TMEM_COLS / BN;
+  static constexpr int N_BARS = 2 * STAGES + 2 * BUFS + 2 * RING + 1;  // full, empty, tfull, tempty, sfull, sempty, drain
   static constexpr int OFF_BARS = STAGES * STAGE_BYTES;
   static constexpr int OFF_SLOT = OFF_BARS + N_BARS * 8;
   static constexpr int OFF_PREFIX = OFF_SLOT + 16;
   static constexpr int OFF_ROW0 = OFF_PREFIX + (MAX_GROUPS + 1) * 4;
-  static constexpr int OFF_MAX = OFF_ROW0 + (MAX_GROUPS + 1) * 4;  // [2 halves of 64][128 rows] magnitudes
+  static constexpr int OFF_CNT = OFF_ROW0 + (MAX_GROUPS + 1) * 4;
+  static constexpr int OFF_MAX = OFF_CNT + MAX_GROUPS * 4;  // [2 halves of 64][128 rows] magnitudes
   static constexpr int MAX_BYTES = QUANT ? 2 * BM * 4 : 0;
-  // staging per warp: 32 rows of 128 bytes (STORE) or 64 bytes (QUANT)
-  static constexpr int STG_ROW = QUANT ? 64 : 128;
-  static constexpr int OFF_STG = (OFF_MAX + MAX_BYTES + 127) / 128 * 128;
+  static constexpr int OFF_RING = (OFF_MAX + MAX_BYTES + 15) / 16 * 16;  // [RING][RING_GROUP]
+  static constexpr int STG_ROW = QUANT || !PAIR ? 64 : 128;  // staging per warp: 32 rows of so many bytes
+  static constexpr int OFF_DST = OFF_RING + RING * RING_GROUP * 4;  // STORE: [sum warp][32] destination rows, factors
+  static constexpr int OFF_STG = (OFF_DST + (QUANT ? 0 : SUM_WARPS * 32 * 8) + 127) / 128 * 128;
   static constexpr int SMEM = 1024 + OFF_STG + SUM_WARPS * 32 * STG_ROW;
+  static_assert((OFF_BARS + 2 * STAGES * 8) % 16 == 0 && BUFS == 2, "the buffers' barriers, see the sums");
   static_assert(OFF_BARS % 8 == 0 && SMEM <= 232448, "shared memory per CTA");
 };
 
@@ -126,13 +144,17 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::OFF_BARS);
   uint64_t* empty = full + STAGES;
   uint64_t* tfull = empty + STAGES;
-  uint64_t* tempty = tfull + 2;
-  uint64_t* drain = tempty + 2;
+  uint64_t* tempty = tfull + C::BUFS;
+  uint64_t* sfull = tempty + C::BUFS;
+  uint64_t* sempty = sfull + RING;
+  uint64_t* drain = sempty + RING;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::OFF_SLOT);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* tile_prefix = reinterpret_cast<int*>(smem + C::OFF_PREFIX);
   int* row0 = reinterpret_cast<int*>(smem + C::OFF_ROW0);
+  int* row_cnt = reinterpret_cast<int*>(smem + C::OFF_CNT);
   float* s_max = reinterpret_cast<float*>(smem + C::OFF_MAX);
+  float* ring = reinterpret_cast<float*>(smem + C::OFF_RING);
 
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
@@ -147,9 +169,13 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
       mbar_init(smem_u32(&full[s]), 1);
       mbar_init(smem_u32(&empty[s]), 1);
     }
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < C::BUFS; ++b) {
       mbar_init(smem_u32(&tfull[b]), 1);
       mbar_init(smem_u32(&tempty[b]), PAIR ? 2 * SUM_WARPS : SUM_WARPS);
+    }
+    for (int r = 0; r < RING; ++r) {
+      mbar_init(smem_u32(&sfull[r]), 32);
+      mbar_init(smem_u32(&sempty[r]), SUM_WARPS);
     }
     mbar_init(smem_u32(drain), 1);
     *abort_flag = 0;
@@ -174,6 +200,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
             }
           }
           row0[g] = r0;
+          row_cnt[g] = mg;
           return (mg + C::TILE_M - 1) / C::TILE_M;
         },
         tile_prefix);
@@ -207,68 +234,68 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
   const int n_kb = p.n_kb;
   const long long budget = p.timeout;
 
-  if (warp == 0) {
-    // ---------------------------------------------------------------- producer
-    const bool issue = elect_one();
-    int stage = 0;
-    uint32_t phase = 0;
-    uint32_t issued = 0;  // bit s: stage s holds a copy the consumer has not released
-    uint32_t issued_phase = 0;
-    int cursor = 0;
-    bool ok = true;
-    for (int tile = tile_first; tile < n_tiles && ok; tile += tile_step) {
-      const TileCoord tc = decode_tile(tile, tile_prefix, p.n_tiles_n, cursor);
-      const int a_row = row0[tc.g] + tc.m_blk * C::TILE_M + static_cast<int>(rank) * BM;
-      const int b_row = tc.g * p.N + tc.n_blk * C::OUT_COLS;
-      for (int kb = 0; kb < n_kb; ++kb) {
-        if (!__all_sync(0xffffffffu,
-                        mbar_wait(smem_u32(&empty[stage]), phase ^ 1u, budget, abort_flag, &g_fp8_error))) {
-          ok = false;
-          break;
+  if (warp < FIRST_SUM) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_FEW));
+    if (warp == 0) {
+      // ---------------------------------------------------------------- producer
+      const bool issue = elect_one();
+      int stage = 0;
+      uint32_t phase = 0;
+      uint32_t issued = 0;  // bit s: stage s holds a copy the consumer has not released
+      uint32_t issued_phase = 0;
+      int cursor = 0;
+      bool ok = true;
+      for (int tile = tile_first; tile < n_tiles && ok; tile += tile_step) {
+        const TileCoord tc = decode_tile(tile, tile_prefix, p.n_tiles_n, cursor);
+        const int a_row = row0[tc.g] + tc.m_blk * C::TILE_M + static_cast<int>(rank) * BM;
+        const int b_row = tc.g * p.N + tc.n_blk * C::OUT_COLS;
+        for (int kb = 0; kb < n_kb; ++kb) {
+          if (!__all_sync(0xffffffffu,
+                          mbar_wait(smem_u32(&empty[stage]), phase ^ 1u, budget, abort_flag, &g_fp8_error))) {
+            ok = false;
+            break;
+          }
+          const uint32_t fb = smem_u32(&full[stage]);
+          const uint32_t da = smem_u32(sA + stage * C::A_BYTES);
+          const uint32_t db = smem_u32(sB + stage * C::B_BYTES);
+          if (!issue) {
+          } else if (PAIR) {
+            // both halves complete on the even CTA's full barrier; of the B tile
+            // the even CTA stages the first half of the columns, the odd CTA the second
+            if (rank == 0) mbar_expect_tx(fb, 2 * C::STAGE_BYTES);
+            const uint32_t fb0 = rank == 0 ? fb : map_to_rank(fb, 0);
+            tma_load_2d_to_pair_bar(da, &tmA, kb * BK, a_row, fb0);
+            tma_load_2d_to_pair_bar(db, MODE == QUANT_SWIGLU && rank ? &tmB2 : &tmB, kb * BK,
+                                    b_row + (MODE == QUANT_SWIGLU ? 0 : static_cast<int>(rank) * HALF), fb0);
+          } else {
+            mbar_expect_tx(fb, C::STAGE_BYTES);
+            tma_load_2d(da, &tmA, kb * BK, a_row, fb);
+            tma_load_2d(db, &tmB, kb * BK, b_row, fb);
+            tma_load_2d(db + HALF * BK, MODE == QUANT_SWIGLU ? &tmB2 : &tmB, kb * BK,
+                        b_row + (MODE == QUANT_SWIGLU ? 0 : HALF), fb);
+          }
+          issued |= 1u << stage;
+          issued_phase = (issued_phase & ~(1u << stage)) | (phase << stage);
+          if (++stage == STAGES) {
+            stage = 0;
+            phase ^= 1u;
+          }
         }
-        const uint32_t fb = smem_u32(&full[stage]);
-        const uint32_t da = smem_u32(sA + stage * C::A_BYTES);
-        const uint32_t db = smem_u32(sB + stage * C::B_BYTES);
-        if (!issue) {
-        } else if (PAIR) {
-          // both halves complete on the even CTA's full barrier; of the B tile
-          // the even CTA stages the first half of the columns, the odd CTA the second
-          if (rank == 0) mbar_expect_tx(fb, 2 * C::STAGE_BYTES);
-          const uint32_t fb0 = rank == 0 ? fb : map_to_rank(fb, 0);
-          tma_load_2d_to_pair_bar(da, &tmA, kb * BK, a_row, fb0);
-          const CUtensorMap* tb = (MODE == QUANT_SWIGLU && rank) ? &tmB2 : &tmB;
-          tma_load_2d_to_pair_bar(db, tb, kb * BK,
-                                  b_row + (MODE == QUANT_SWIGLU ? 0 : static_cast<int>(rank) * HALF), fb0);
+      }
+      if (!ok || *abort_flag) {
+        // Let every copy this CTA started land before shared memory is released.
+        if (PAIR && rank != 0) {
+          // its copies complete on the even CTA's barriers: wait a fixed time
+          if (issued) {
+            const unsigned long long t0 = globaltimer_ns();
+            while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
+          }
         } else {
-          mbar_expect_tx(fb, C::STAGE_BYTES);
-          tma_load_2d(da, &tmA, kb * BK, a_row, fb);
-          tma_load_2d(db, &tmB, kb * BK, b_row, fb);
-          tma_load_2d(db + HALF * BK, MODE == QUANT_SWIGLU ? &tmB2 : &tmB, kb * BK,
-                      b_row + (MODE == QUANT_SWIGLU ? 0 : HALF), fb);
-        }
-        issued |= 1u << stage;
-        issued_phase = (issued_phase & ~(1u << stage)) | (phase << stage);
-        if (++stage == STAGES) {
-          stage = 0;
-          phase ^= 1u;
+          for (int s = 0; s < STAGES; ++s)
+            if (issued & (1u << s)) mbar_drain(smem_u32(&full[s]), (issued_phase >> s) & 1u, DRAIN_CYCLES);
         }
       }
-    }
-    if (!ok || *abort_flag) {
-      // Let every copy this CTA started land before shared memory is released.
-      if (PAIR && rank != 0) {
-        // its copies complete on the even CTA's barriers: wait a fixed time
-        if (issued) {
-          const unsigned long long t0 = globaltimer_ns();
-          while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
-        }
-      } else {
-        for (int s = 0; s < STAGES; ++s)
-          if (issued & (1u << s)) mbar_drain(smem_u32(&full[s]), (issued_phase >> s) & 1u, DRAIN_CYCLES);
-      }
-    }
-  } else if (warp == 1) {
-    if (!PAIR || rank == 0) {
+    } else if (warp == 1 && (!PAIR || rank == 0)) {
       // -------------------------------------------------------------- MMA issuer
       const bool issue = elect_one();
       constexpr uint32_t IDESC = idesc_e4m3(C::TILE_M, BN);
@@ -276,16 +303,16 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
       const uint64_t db0 = sdesc_sw128(smem_u32(sB));
       int stage = 0;
       uint32_t phase = 0;
-      uint32_t it = 0;  // blocks so far: buffer it & 1, phase (it >> 1) & 1
+      uint32_t it = 0;  // blocks so far: buffer it & 1, its phase (it >> 1) & 1
       bool ok = true, any = false;
       for (int tile = tile_first; tile < n_tiles && ok; tile += tile_step) {
         for (int kb = 0; kb < n_kb; ++kb, ++it) {
           const uint32_t buf = it & 1u, bph = (it >> 1) & 1u;
-          const bool freed =
-              PAIR ? mbar_wait_cluster(smem_u32(&tempty[buf]), bph ^ 1u, budget, abort_flag, &g_fp8_error)
-                   : mbar_wait(smem_u32(&tempty[buf]), bph ^ 1u, budget, abort_flag, &g_fp8_error);
-          if (!__all_sync(0xffffffffu, freed && mbar_wait(smem_u32(&full[stage]), phase, budget, abort_flag,
-                                                          &g_fp8_error))) {
+          // the operands first: they are there while the buffer is still being read
+          const bool there = mbar_wait(smem_u32(&full[stage]), phase, budget, abort_flag, &g_fp8_error);
+          if (!__all_sync(0xffffffffu,
+                          there && (PAIR ? mbar_wait_cluster(smem_u32(&tempty[buf]), bph ^ 1u, budget, abort_flag, &g_fp8_error)
+                                         : mbar_wait(smem_u32(&tempty[buf]), bph ^ 1u, budget, abort_flag, &g_fp8_error)))) {
             ok = false;
             break;
           }
@@ -303,11 +330,11 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
               else umma_fp8(d, da + 2 * kk, db + 2 * kk, IDESC, kk ? 1u : 0u);
             }
             if (PAIR) {
-              umma_commit_pair_mc(smem_u32(&empty[stage]));
               umma_commit_pair_mc(smem_u32(&tfull[buf]));
+              umma_commit_pair_mc(smem_u32(&empty[stage]));
             } else {
-              umma_commit(smem_u32(&empty[stage]));
               umma_commit(smem_u32(&tfull[buf]));
+              umma_commit(smem_u32(&empty[stage]));
             }
           }
           any = true;
@@ -323,69 +350,138 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
         else umma_commit(smem_u32(drain));
         mbar_drain(smem_u32(drain), 0, DRAIN_CYCLES);
       }
+    } else if (warp == 2) {
+      // ------------------------------------------------------------------ scales
+      // Asynchronous copies, as far ahead as the ring is deep: a row's SG scales at
+      // once where they are aligned to that.  A copy takes the load path a turn per
+      // row, which the barriers share; copies of single scales held up the sums
+      // (16384 x 14336 x 4096: 846 us, without them 717).
+      const uint32_t ring0 = smem_u32(ring);
+      uint32_t it = 0;
+      int cursor = 0;
+      bool ok = true;
+      for (int tile = tile_first; tile < n_tiles && ok; tile += tile_step) {
+        const TileCoord tc = decode_tile(tile, tile_prefix, p.n_tiles_n, cursor);
+        const int mg = row_cnt[tc.g];
+        const int left = mg - tc.m_blk * C::TILE_M - static_cast<int>(rank) * BM - lane;  // > 32 i: row lane + 32 i exists
+        const float* sa = p.SA + (static_cast<long long>(row0[tc.g]) + mg - left) * p.sa_pitch;
+        // lanes 0 and 1: the two halves' column blocks (a half beyond N: the last
+        // block's, its columns are not stored)
+        int nb = MODE == QUANT_SWIGLU ? tc.n_blk : 2 * tc.n_blk + (lane & 1);
+        if (nb >= p.n_nb) nb = p.n_nb - 1;
+        const float* sb =
+            (MODE == QUANT_SWIGLU && (lane & 1) ? p.SB2 : p.SB) + (static_cast<long long>(tc.g) * p.n_nb + nb) * n_kb;
+        for (int kb0 = 0; kb0 < n_kb; kb0 += SG, ++it) {
+          const uint32_t slot = it % RING, sph = (it / RING) & 1u;
+          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sempty[slot]), sph ^ 1u, budget, abort_flag, &g_fp8_error));
+          if (!ok) break;
+          const uint32_t to = ring0 + slot * (RING_GROUP * 4);
+          const int n = n_kb - kb0 < SG ? n_kb - kb0 : SG;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (left <= 32 * i) continue;
+            const float* from = sa + static_cast<long long>(32 * i) * p.sa_pitch + kb0;
+            const uint32_t at = to + 16 * (lane + 32 * i);
+            if (n == SG && p.sa_words == 4) {
+              cp_async<16>(at, from);
+            } else if (n == SG && p.sa_words == 2) {
+              cp_async<8>(at, from);
+              cp_async<8>(at + 8, from + 2);
+            } else {
+              for (int u = 0; u < n; ++u) cp_async<4>(at + 4 * u, from + u);
+            }
+          }
+          if (lane < 2)
+            for (int u = 0; u < n; ++u) cp_async<4>(to + 16 * BM + 4 * (2 * u + lane), sb + kb0 + u);
+          cp_async_arrive(smem_u32(&sfull[slot]));
+        }
+      }
+      cp_async_wait();  // none in flight when shared memory is released
     }
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SUM));
     // ------------------------------------------------------ sums and epilogue
-    const int q = warp & 3;              // TMEM lane quadrant this warp may read
-    const int part = (warp - 2) >> 2;    // which 64 columns of each half
+    const int q = warp & 3;                    // TMEM lane quadrant this warp may read
+    const int part = (warp - FIRST_SUM) >> 2;  // which 64 columns of each half
     const int row_in_tile = q * 32 + lane;
     const uint32_t t_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + part * 64;
     const uint32_t release0 = PAIR ? map_to_rank(smem_u32(&tempty[0]), 0) : smem_u32(&tempty[0]);
-    uint8_t* stg = smem + C::OFF_STG + (warp - 2) * 32 * C::STG_ROW;
-    uint32_t it = 0;
+    uint8_t* stg = smem + C::OFF_STG + (warp - FIRST_SUM) * 32 * C::STG_ROW;
+    int2* s_dst = reinterpret_cast<int2*>(smem + C::OFF_DST) + (warp - FIRST_SUM) * 32;
+    // the buffer in turn: its columns, its barriers (8 bytes apart, pairs aligned
+    // to 16) and its phase
+    uint32_t t_at = t_row, full_at = smem_u32(&tfull[0]), release_at = release0, bph = 0;
+    uint32_t slot = 0, sph = 0;  // of the scales
     int cursor = 0;
     bool ok = true;
     for (int tile = tile_first; tile < n_tiles; tile += tile_step) {
       const TileCoord tc = decode_tile(tile, tile_prefix, p.n_tiles_n, cursor);
-      const int mg = p.offsets ? p.offsets[tc.g + 1] - p.offsets[tc.g] : p.rows;
+      const int mg = row_cnt[tc.g];
       const int local = tc.m_blk * C::TILE_M + static_cast<int>(rank) * BM + row_in_tile;
       const bool valid = local < mg;
       const long long row = static_cast<long long>(row0[tc.g]) + local;
-      const float* sa = p.SA + row * n_kb;
-      // the scales of the two halves' column blocks (a half beyond N: the last
-      // block's, its columns are not stored)
-      const int nb0 = MODE == QUANT_SWIGLU ? tc.n_blk : 2 * tc.n_blk;
-      const int nb1 = MODE == QUANT_SWIGLU ? tc.n_blk : (2 * tc.n_blk + 1 < p.n_nb ? 2 * tc.n_blk + 1 : nb0);
-      const float* sb0 = p.SB + (static_cast<long long>(tc.g) * p.n_nb + nb0) * n_kb;
-      const float* sb1 =
-          (MODE == QUANT_SWIGLU ? p.SB2 : p.SB) + (static_cast<long long>(tc.g) * p.n_nb + nb1) * n_kb;
-      uint64_t acc[2][32];
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < 32; ++i) acc[h][i] = 0;
-      // scales one block ahead
-      float a_next = valid ? sa[0] : 0.0f, b0_next = sb0[0], b1_next = sb1[0];
-      for (int kb = 0; kb < n_kb && ok; ++kb, ++it) {
-        const uint32_t buf = it & 1u, bph = (it >> 1) & 1u;
-        const float f0 = a_next * b0_next, f1 = a_next * b1_next;
-        if (kb + 1 < n_kb) {
-          a_next = valid ? sa[kb + 1] : 0.0f;
-          b0_next = sb0[kb + 1];
-          b1_next = sb1[kb + 1];
+      if (!C::QUANT) {
+        // where the row goes (-1: nowhere) and its factor, read while the first
+        // block is multiplied and kept out of the registers meanwhile
+        int dest = valid ? static_cast<int>(row) : -1;
+        float sc = 1.0f;
+        if (valid && p.perm) {
+          dest = p.perm[row];
+          if (dest < 0 || dest >= p.rows) {
+            atomicOr(&g_fp8_error, 2u);
+            dest = -1;
+          } else if (p.row_scale) {
+            sc = p.row_scale[dest];
+          }
         }
-        const uint64_t ff[2] = {f32x2(f0, f0), f32x2(f1, f1)};
-        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&tfull[buf]), bph, budget, abort_flag, &g_fp8_error));
+        s_dst[lane] = make_int2(dest, __float_as_int(sc));
+      }
+      float acc[2][64];
+#pragma unroll
+      for (int i = 0; i < 128; ++i) acc[i >> 6][i & 63] = 0.0f;
+      for (int kb0 = 0; kb0 < n_kb && ok; kb0 += SG) {
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sfull[slot]), sph, budget, abort_flag, &g_fp8_error));
         if (!ok) break;
-        tc_fence_after();
-        const uint32_t t0 = t_row + buf * BN;
-        // pieces of 16 columns, one in flight while the one before is added
-        uint32_t r[2][16];
-        tmem_ld16_nw(t0, r[0]);
+        // the group's scales to registers (of rows that do not exist: anything,
+        // their sums are not stored)
+        const float* scales = ring + slot * RING_GROUP;
+        float a[SG];
+        *reinterpret_cast<float4*>(a) = *reinterpret_cast<const float4*>(scales + SG * row_in_tile);
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          tmem_wait_for16(r[c & 1]);
-          if (c + 1 < 8) tmem_ld16_nw(t0 + ((c + 1) >> 2) * HALF + ((c + 1) & 3) * 16, r[(c + 1) & 1]);
+        for (int u = 0; u < SG; ++u) {
+          if (kb0 + u >= n_kb) break;
+          const float2 b = *reinterpret_cast<const float2*>(scales + SG * BM + 2 * u);
+          ok = __all_sync(0xffffffffu, mbar_wait(full_at, bph, budget, abort_flag, &g_fp8_error));
+          if (!ok) break;
+          tc_fence_after();
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            acc[c >> 2][(c & 3) * 8 + i] =
-                f32x2_fma(f32x2_bits(r[c & 1][2 * i], r[c & 1][2 * i + 1]), ff[c >> 2], acc[c >> 2][(c & 3) * 8 + i]);
+          for (int h = 0; h < 2; ++h) {
+            float r[64];
+            tmem_ld64(t_at + h * HALF, r);
+            if (h == 1) {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) {
+                if (PAIR) mbar_arrive_remote(release_at);
+                else mbar_arrive(release_at);
+              }
+              // the other buffer; both have been used once more after the second
+              bph ^= (t_at / BN) & 1u;
+              t_at ^= BN;
+              full_at ^= 8u;
+              release_at ^= 8u;
+            }
+            const float f = a[u] * (h ? b.y : b.x);
+#pragma unroll
+            for (int i = 0; i < 64; ++i) acc[h][i] = fmaf(r[i], f, acc[h][i]);
+          }
         }
-        tc_fence_before();
+        // the group's scales have been read
         __syncwarp();
-        if (lane == 0) {
-          if (PAIR) mbar_arrive_remote(release0 + 8 * buf);
-          else mbar_arrive(release0 + 8 * buf);
+        if (lane == 0) mbar_arrive(smem_u32(&sempty[slot]));
+        if (++slot == RING) {
+          slot = 0;
+          sph ^= 1u;
         }
       }
       if (C::QUANT) {
@@ -406,37 +502,27 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
 #pragma unroll
         for (int h = 0; h < BLOCKS; ++h) {
           const int col0 = tc.n_blk * C::OUT_COLS + h * HALF + part * 64;
-          float v[64];
           float m = 0.0f;
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            float2 u = f32x2_get(acc[h][i]);
-            if (MODE == QUANT_SWIGLU) {
-              const float2 w = f32x2_get(acc[1][i]);
-              u.x = silu_bf16out(u.x) * w.x;
-              u.y = silu_bf16out(u.y) * w.y;
-            } else {
-              u.x = gelu_erf(u.x);
-              u.y = gelu_erf(u.y);
-            }
-            v[2 * i] = u.x;
-            v[2 * i + 1] = u.y;
+          for (int i = 0; i < 64; ++i) {
+            acc[h][i] = MODE == QUANT_SWIGLU ? silu_bf16out(acc[h][i]) * acc[1][i] : gelu_erf(acc[h][i]);
             // columns beyond N belong to other weights: not part of the block
-            if (col0 + 2 * i < p.N) m = fmaxf(m, fmaxf(fabsf(u.x), fabsf(u.y)));
+            if (col0 + i < p.N) m = fmaxf(m, fabsf(acc[h][i]));
           }
           s_max[part * BM + row_in_tile] = m;
           asm volatile("bar.sync %0, 64;" ::"r"(1 + q) : "memory");
           m = fmaxf(m, s_max[(part ^ 1) * BM + row_in_tile]);
           const Fp8Scale f = fp8_scale(m);
           const int nb = tc.n_blk * BLOCKS + h;
-          if (valid && part == 0 && nb < p.n_nb) p.out_scale[row * p.n_nb + nb] = f.scale;
+          if (valid && part == 0 && nb < p.n_nb) p.out_scale[row * p.out_scale_pitch + nb] = f.scale;
           __syncwarp();
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            *reinterpret_cast<U4*>(stg + lane * 64 + ((j ^ ((lane >> 1) & 3)) * 16)) = fp8_pack16(v + 16 * j, f.inv);
+            *reinterpret_cast<U4*>(stg + lane * 64 + ((j ^ ((lane >> 1) & 3)) * 16)) =
+                fp8_pack16(&acc[h][16 * j], f.inv);
           __syncwarp();
           uint8_t* o = static_cast<uint8_t*>(p.out) + col0;
-#pragma unroll
+#pragma unroll 1
           for (int pass = 0; pass < 4; ++pass) {
             const int rr = pass * 8 + (lane >> 2);
             const int seg = lane & 3;
@@ -448,58 +534,43 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
           asm volatile("bar.sync %0, 64;" ::"r"(1 + q) : "memory");
         }
       } else {
+        // Slabs of SLAB columns: rounded into the warp's staging rows (16-byte
+        // chunks XOR-swizzled by row), then stored as whole row segments.  The
+        // storing loop is rolled: this code runs once per tile, and fetching it
+        // is what it takes longest for.
         constexpr int ES = MODE == STORE_F32 ? 4 : 2;
-        constexpr int SLAB = 128 / ES;  // columns of one 128-byte row segment
-        long long dest = row;
-        float sc = 1.0f;
-        bool put = valid;
-        if (valid && p.perm) {
-          dest = p.perm[row];
-          if (dest < 0 || dest >= p.rows) {
-            atomicOr(&g_fp8_error, 2u);
-            put = false;
-            dest = 0;
-          } else if (p.row_scale) {
-            sc = p.row_scale[dest];
+        constexpr int SLAB = C::STG_ROW / ES, SEGS = C::STG_ROW / 16;
+        constexpr int SHIFT = SEGS == 4 ? 1 : 0;
+        const float sc = __int_as_float(s_dst[lane].y);
+#pragma unroll
+        for (int c = 0; c < 128; c += SLAB) {
+          __syncwarp();
+#pragma unroll
+          for (int j = 0; j < SEGS; ++j) {
+            U4 x;
+            if (MODE == STORE_F32) {
+              const float* v = &acc[(c + 4 * j) >> 6][(c + 4 * j) & 63];
+              x = U4{__float_as_uint(v[0] * sc), __float_as_uint(v[1] * sc), __float_as_uint(v[2] * sc),
+                     __float_as_uint(v[3] * sc)};
+            } else {
+              const float* v = &acc[((c + 8 * j) >> 6) & 1][(c + 8 * j) & 63];
+              x = U4{pack_bf16x2(v[0] * sc, v[1] * sc), pack_bf16x2(v[2] * sc, v[3] * sc),
+                     pack_bf16x2(v[4] * sc, v[5] * sc), pack_bf16x2(v[6] * sc, v[7] * sc)};
+            }
+            *reinterpret_cast<U4*>(stg + lane * C::STG_ROW + ((j ^ ((lane >> SHIFT) & (SEGS - 1))) * 16)) = x;
+          }
+          __syncwarp();
+          const int seg = lane & (SEGS - 1);
+          const int col = tc.n_blk * BN + (c >> 6) * HALF + part * 64 + (c & 63) + seg * (16 / ES);
+#pragma unroll 1
+          for (int rr = lane / SEGS; rr < 32; rr += 32 / SEGS) {
+            const U4 x = *reinterpret_cast<const U4*>(stg + rr * C::STG_ROW + ((seg ^ ((rr >> SHIFT) & (SEGS - 1))) * 16));
+            const int drow = s_dst[rr].x;
+            if (drow >= 0 && col < p.N)
+              *reinterpret_cast<U4*>(static_cast<uint8_t*>(p.out) + (drow * p.ldo + col) * ES) = x;
           }
         }
-        const unsigned pmask = __ballot_sync(0xffffffffu, put);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-#pragma unroll
-          for (int sl = 0; sl < 64 / SLAB; ++sl) {
-            const int col0 = tc.n_blk * BN + h * HALF + part * 64 + sl * SLAB;
-            __syncwarp();
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              U4 x;
-              uint32_t w[4];
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                if (MODE == STORE_F32) {
-                  const float2 u = f32x2_get(acc[h][sl * 16 + j * 2 + (i >> 1)]);
-                  w[i] = __float_as_uint((i & 1 ? u.y : u.x) * sc);
-                } else {
-                  const float2 u = f32x2_get(acc[h][(j * 4 + i) & 31]);
-                  w[i] = pack_bf16x2(u.x * sc, u.y * sc);
-                }
-              }
-              x = U4{w[0], w[1], w[2], w[3]};
-              *reinterpret_cast<U4*>(stg + lane * 128 + ((j ^ (lane & 7)) * 16)) = x;
-            }
-            __syncwarp();
-            const int seg = lane & 7;
-            const int col = col0 + seg * (16 / ES);
-#pragma unroll
-            for (int pass = 0; pass < 8; ++pass) {
-              const int rr = pass * 4 + (lane >> 3);
-              const U4 x = *reinterpret_cast<const U4*>(stg + rr * 128 + ((seg ^ (rr & 7)) * 16));
-              const long long drow = __shfl_sync(0xffffffffu, dest, rr);
-              if (((pmask >> rr) & 1u) && col < p.N)
-                *reinterpret_cast<U4*>(static_cast<uint8_t*>(p.out) + (drow * p.ldo + col) * ES) = x;
-            }
-          }
-        }
+        __syncwarp();
       }
     }
   }
@@ -535,6 +606,10 @@ cudaError_t launch_cfg(const Fp8GemmArgs& a, cudaStream_t s) {
   if (MODE == QUANT_SWIGLU && !make_tensor_map_u8(&mB2, a.B2, b_rows, a.K, HALF)) return cudaErrorInvalidValue;
   Params p;
   p.SA = a.SA;
+  p.sa_pitch = a.sa_pitch > 0 ? a.sa_pitch : (a.K + BK - 1) / BK;
+  p.sa_words = 1;
+  for (int w = 4; w > 1 && p.sa_words == 1; w /= 2)
+    if (p.sa_pitch % w == 0 && reinterpret_cast<uintptr_t>(a.SA) % (4 * w) == 0) p.sa_words = w;
   p.SB = a.SB;
   p.SB2 = a.SB2;
   p.offsets = a.offsets;
@@ -548,6 +623,7 @@ cudaError_t launch_cfg(const Fp8GemmArgs& a, cudaStream_t s) {
   p.out = a.out;
   p.ldo = a.ldo;
   p.out_scale = a.out_scale;
+  p.out_scale_pitch = a.out_scale_pitch;
   p.perm = a.perm;
   p.row_scale = a.row_scale;
   p.timeout = a.timeout_cycles;

@@ -292,6 +292,7 @@ cudaError_t read_quant_error(unsigned int* word);
 struct Fp8GemmArgs {
   const void* A;
   const float* SA;
+  int sa_pitch;         // floats per row of SA (0: ceil(K / 128))
   const void* B;
   const float* SB;
   const void* B2;       // SwiGLU: W3
@@ -302,6 +303,7 @@ struct Fp8GemmArgs {
   long long ldo;        // EPI_STORE: pitch in elements
   bool out_bf16;
   float* out_scale;
+  int out_scale_pitch;  // floats per row of out_scale
   const int32_t* perm;
   const float* row_scale;
   int g_active;         // groups expected to hold rows (0 = G)
