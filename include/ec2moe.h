@@ -364,7 +364,8 @@ ec2moe_status ec2moe_fp8_quantize(int32_t dtype, int32_t n_mats, int32_t rows, i
                                   const void* X, int32_t block_rows, const int32_t* inv_perm, int32_t k, void* Q,
                                   float* scale, ec2moe_stream_t stream);
 
-/* Bytes of device workspace ec2moe_fp8_gemm needs (0: none, or an invalid size). */
+/* Bytes of device workspace ec2moe_fp8_gemm needs on the current device (0: none,
+ * or an invalid size): partial sums of calls with few rows per group. */
 size_t ec2moe_fp8_gemm_workspace_size(int32_t n_groups, int32_t rows, int32_t N, int32_t K);
 
 /* C_g = A_g B_g^T of 8-bit operands: group g owns the rows [offsets[g],
@@ -396,7 +397,8 @@ typedef struct ec2moe_fp8_weights {
   const float* S2;
 } ec2moe_fp8_weights;
 
-/* Bytes of device workspace ec2moe_experts_fp8 needs (hidden rows and scales). */
+/* Bytes of device workspace ec2moe_experts_fp8 needs on the current device (hidden
+ * rows and their scales; partial sums where an expert's rows are few). */
 size_t ec2moe_experts_fp8_workspace_size(const ec2moe_layer_desc* desc);
 
 /* ec2moe_experts on 8-bit rows and weights.
@@ -478,7 +480,7 @@ int32_t ec2moe_last_launch_count(void);
  * "lr_encode", "lr_reduce", "lr_decode", "lr_codec", "expert_up", "expert_down", "shared_up",
  * "shared_down", "ffn_up", "ffn_down" (routed and shared experts in one launch),
  * "combine", "sum_counts", "quantize_rows", "quantize_blocks", "fp8_gemm", "fp8_up",
- * "fp8_down", "logits_prep", "logits_gemm", "logits_sum", "balance_clear",
+ * "fp8_down", "fp8_sum", "logits_prep", "logits_gemm", "logits_sum", "balance_clear",
  * "balance_count", "balance_main", "balance_final"); `ms` its device duration.  Profiling is off by default and
  * costs nothing when off. */
 ec2moe_status ec2moe_profile_enable(int32_t enable);

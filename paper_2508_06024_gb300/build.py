@@ -19,7 +19,7 @@ OUT_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libec2moe.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 SOURCES = ["api.cu", "gate.cu", "gate_tc.cu", "route.cu", "tc_gemm.cu", "f32_gemm.cu", "tok_gemm.cu", "codec.cu", "skinny.cu", "tc_swap.cu",
-           "fp8_quant.cu", "fp8_gemm.cu", "gate_logits.cu", "balance.cu", "sched.cpp"]
+           "fp8_quant.cu", "fp8_gemm.cu", "fp8_swap.cu", "gate_logits.cu", "balance.cu", "sched.cpp"]
 
 
 def nvcc() -> str:

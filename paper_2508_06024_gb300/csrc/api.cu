@@ -586,10 +586,15 @@ ec2moe_status check_fp8_experts(const ec2moe_layer_desc* d) {
   return st != EC2MOE_OK ? st : check_fp8_shape(d->E, rows, d->d, d->d_ff);
 }
 
+cudaError_t run_fp8(const Fp8GemmArgs& g, int epi, cudaStream_t s) {
+  return fp8_swap_rows(g.G, g.rows, g.N, epi == EPI_SWIGLU ? 2 : 1) ? launch_gemm_fp8_swap(g, epi, s) : launch_gemm_fp8(g, epi, s);
+}
+
 // Workspace of ec2moe_experts_fp8: hidden rows (at 0), their scales (a row's
-// padded to 16 bytes, so that the down projection copies four at once).
+// padded to 16 bytes, so that the down projection copies four at once), partial
+// sums of calls with few rows per expert.
 struct Fp8Ws {
-  size_t hs, total;
+  size_t hs, part, total;
   int hs_pitch;
 };
 Fp8Ws fp8_ws(const ec2moe_layer_desc* d) {
@@ -597,7 +602,10 @@ Fp8Ws fp8_ws(const ec2moe_layer_desc* d) {
   Fp8Ws w;
   w.hs_pitch = ((d->d_ff + EC2MOE_FP8_BLOCK - 1) / EC2MOE_FP8_BLOCK + 3) / 4 * 4;
   w.hs = align_up(rows * d->d_ff);
-  w.total = w.hs + align_up(rows * w.hs_pitch * 4);
+  w.part = w.hs + align_up(rows * w.hs_pitch * 4);
+  const size_t up = fp8_swap_bytes(d->E, (int)rows, d->d_ff, d->act == EC2MOE_SWIGLU ? 2 : 1);
+  const size_t down = fp8_swap_bytes(d->E, (int)rows, d->d, 1);
+  w.total = w.part + align_up(up > down ? up : down);
   return w;
 }
 
@@ -1133,7 +1141,7 @@ ec2moe_status ec2moe_fp8_quantize(int32_t dtype, int32_t n_mats, int32_t rows, i
 
 size_t ec2moe_fp8_gemm_workspace_size(int32_t n_groups, int32_t rows, int32_t N, int32_t K) {
   if (check_fp8_shape(n_groups, rows, N, K) != EC2MOE_OK) return 0;
-  return 0;
+  return align_up(fp8_swap_bytes(n_groups, rows, N, 1));
 }
 
 ec2moe_status ec2moe_fp8_gemm(int32_t n_groups, int32_t rows, int32_t N, int32_t K, const void* A,
@@ -1151,8 +1159,9 @@ ec2moe_status ec2moe_fp8_gemm(int32_t n_groups, int32_t rows, int32_t N, int32_t
   EC2MOE_REQUIRE_PTR(B);
   EC2MOE_REQUIRE_PTR(C);
   if (!A_scale || !B_scale) return EC2MOE_ERR_INVALID_ARG;
-  (void)workspace;
-  (void)ws_bytes;
+  const size_t need = ec2moe_fp8_gemm_workspace_size(n_groups, rows, N, K);
+  if (need > 0 && (!workspace || ws_bytes < need)) return EC2MOE_ERR_WORKSPACE;
+  if (need > 0 && !aligned16(workspace)) return EC2MOE_ERR_MISALIGNED;
   Fp8GemmArgs g{};
   g.timeout_cycles = default_timeout_cycles();
   g.name = "fp8_gemm";
@@ -1168,7 +1177,8 @@ ec2moe_status ec2moe_fp8_gemm(int32_t n_groups, int32_t rows, int32_t N, int32_t
   g.out = C;
   g.ldo = ldc;
   g.out_bf16 = out_dtype == EC2MOE_BF16;
-  EC2MOE_CUDA(launch_gemm_fp8(g, EPI_STORE, stream));
+  g.part = workspace;
+  EC2MOE_CUDA(run_fp8(g, EPI_STORE, stream));
   return EC2MOE_OK;
 }
 
@@ -1214,7 +1224,8 @@ ec2moe_status ec2moe_experts_fp8(const ec2moe_layer_desc* desc, const void* Xq, 
   g.out = ws;
   g.out_scale = reinterpret_cast<float*>(ws + L.hs);
   g.out_scale_pitch = L.hs_pitch;
-  EC2MOE_CUDA(launch_gemm_fp8(g, glu ? EPI_SWIGLU : EPI_GELU, stream));
+  g.part = ws + L.part;
+  EC2MOE_CUDA(run_fp8(g, glu ? EPI_SWIGLU : EPI_GELU, stream));
   g.name = "fp8_down";
   g.A = ws;
   g.SA = g.out_scale;
@@ -1231,7 +1242,7 @@ ec2moe_status ec2moe_experts_fp8(const ec2moe_layer_desc* desc, const void* Xq, 
   g.out_scale = nullptr;
   g.perm = perm;
   g.row_scale = topk_w;
-  EC2MOE_CUDA(launch_gemm_fp8(g, EPI_STORE, stream));
+  EC2MOE_CUDA(run_fp8(g, EPI_STORE, stream));
   return EC2MOE_OK;
 }
 
@@ -1323,8 +1334,8 @@ ec2moe_status ec2moe_balance_loss(const ec2moe_layer_desc* desc, const float* lo
 
 ec2moe_status ec2moe_last_device_error(ec2moe_stream_t stream) {
   if (cudaStreamSynchronize(stream) != cudaSuccess) return EC2MOE_ERR_CUDA;
-  unsigned int tc = 0, codec = 0, gate = 0, route = 0, swap = 0, skinny = 0, f32 = 0, tok = 0, fp8 = 0, quant = 0,
-               balance = 0;
+  unsigned int tc = 0, codec = 0, gate = 0, route = 0, swap = 0, skinny = 0, f32 = 0, tok = 0, fp8 = 0, fp8_swap = 0,
+               quant = 0, balance = 0;
   if (read_tc_error(&tc) != cudaSuccess) return EC2MOE_ERR_CUDA;
   if (read_codec_error(&codec) != cudaSuccess) return EC2MOE_ERR_CUDA;
   if (read_gate_error(&gate) != cudaSuccess) return EC2MOE_ERR_CUDA;
@@ -1334,6 +1345,8 @@ ec2moe_status ec2moe_last_device_error(ec2moe_stream_t stream) {
   if (read_f32_error(&f32) != cudaSuccess) return EC2MOE_ERR_CUDA;
   if (read_tok_error(&tok) != cudaSuccess) return EC2MOE_ERR_CUDA;
   if (read_fp8_error(&fp8) != cudaSuccess) return EC2MOE_ERR_CUDA;
+  if (read_fp8_swap_error(&fp8_swap) != cudaSuccess) return EC2MOE_ERR_CUDA;
+  fp8 |= fp8_swap;
   if (read_quant_error(&quant) != cudaSuccess) return EC2MOE_ERR_CUDA;
   if (read_balance_error(&balance) != cudaSuccess) return EC2MOE_ERR_CUDA;
   // bit 0 of the GEMM, codec and gate words: a bounded wait timed out;
