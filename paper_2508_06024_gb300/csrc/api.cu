@@ -1335,7 +1335,7 @@ ec2moe_status ec2moe_balance_loss(const ec2moe_layer_desc* desc, const float* lo
 ec2moe_status ec2moe_last_device_error(ec2moe_stream_t stream) {
   if (cudaStreamSynchronize(stream) != cudaSuccess) return EC2MOE_ERR_CUDA;
   unsigned int tc = 0, codec = 0, gate = 0, route = 0, swap = 0, skinny = 0, f32 = 0, tok = 0, fp8 = 0, fp8_swap = 0,
-               quant = 0, balance = 0;
+               quant = 0, balance = 0, logits = 0;
   if (read_tc_error(&tc) != cudaSuccess) return EC2MOE_ERR_CUDA;
   if (read_codec_error(&codec) != cudaSuccess) return EC2MOE_ERR_CUDA;
   if (read_gate_error(&gate) != cudaSuccess) return EC2MOE_ERR_CUDA;
@@ -1347,12 +1347,13 @@ ec2moe_status ec2moe_last_device_error(ec2moe_stream_t stream) {
   if (read_fp8_error(&fp8) != cudaSuccess) return EC2MOE_ERR_CUDA;
   if (read_fp8_swap_error(&fp8_swap) != cudaSuccess) return EC2MOE_ERR_CUDA;
   fp8 |= fp8_swap;
+  if (read_logits_error(&logits) != cudaSuccess) return EC2MOE_ERR_CUDA;
   if (read_quant_error(&quant) != cudaSuccess) return EC2MOE_ERR_CUDA;
   if (read_balance_error(&balance) != cudaSuccess) return EC2MOE_ERR_CUDA;
   // bit 0 of the GEMM, codec and gate words: a bounded wait timed out;
   // bit 1 of the GEMM words and any bit of the routing, quantiser and balance
   // words: an index outside the call's rows or experts was skipped
-  if ((tc | codec | gate | swap | f32 | tok | fp8) & 1u) return EC2MOE_ERR_TIMEOUT;
+  if ((tc | codec | gate | swap | f32 | tok | fp8 | logits) & 1u) return EC2MOE_ERR_TIMEOUT;
   if (((tc | swap | skinny | f32 | tok | fp8) & 2u) || route || quant || balance) return EC2MOE_ERR_INVALID_ARG;
   return EC2MOE_OK;
 }

@@ -337,6 +337,7 @@ struct LogitsArgs {
 };
 size_t gate_logits_bytes(int T, int d, int E, int K, bool bf16);
 cudaError_t launch_gate_logits(const LogitsArgs& a, bool bf16, cudaStream_t s);
+cudaError_t read_logits_error(unsigned int* word);  // bit 0: a bounded wait timed out
 
 struct BalanceArgs {
   const float* logits;        // pitch ld
