@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include "common.cuh"
+#include "tc_ptx.cuh"
 
 namespace ec2moe {
 
@@ -37,8 +38,8 @@ __device__ __forceinline__ U4 fp8_pack16(const float* v, float inv) {
 
 namespace tc {
 
-// 32 lanes x 64 columns of fp32 TMEM words: thread i of the warp receives columns
-// [col, col + 64) of TMEM lane (quadrant base + i).  Loads and wait are one
+// 32 lanes x 64 columns of fp32 TMEM words: thread i of the warp receives the
+// columns from taddr's of TMEM lane (quadrant base + i).  Loads and wait are one
 // statement, so nothing that reads the values is moved before the wait.
 __device__ __forceinline__ void tmem_ld64(uint32_t taddr, float* v) {
   asm volatile(
@@ -69,6 +70,20 @@ __device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+// Arrive under a predicate, without a branch.
+__device__ __forceinline__ void mbar_arrive_if(bool on, uint32_t bar) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %1, 0;\n\t@p mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}\n" ::"r"(
+                   bar),
+               "r"(static_cast<uint32_t>(on))
+               : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_remote_if(bool on, uint32_t cluster_addr) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %1, 0;\n\t@p mbarrier.arrive.shared::cluster.b64 _, [%0];\n\t}\n" ::"r"(
+                   cluster_addr),
+               "r"(static_cast<uint32_t>(on))
+               : "memory");
+}
 
 // Instruction descriptor of tcgen05.mma kind::f8f6f4: fp32 accumulator (bits 4-5
 // = 1), A and B e4m3 (bits 7-9 and 10-12 = 0), both K-major, N >> 3 in bits

@@ -107,7 +107,7 @@ template <int MODE, bool PAIR>
 struct Cfg {
   static constexpr bool QUANT = MODE == QUANT_GELU || MODE == QUANT_SWIGLU;
   static constexpr int TILE_M = PAIR ? 2 * BM : BM;
-  static constexpr int B_ROWS = PAIR ? BN / 2 : BN;  // rows of the B tile this CTA stages
+  static constexpr int B_ROWS = PAIR ? HALF : BN;  // rows of the B tile this CTA stages
   static constexpr int A_BYTES = BM * BK;
   static constexpr int B_BYTES = B_ROWS * BK;
   static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
@@ -365,7 +365,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
         const int mg = row_cnt[tc.g];
         const int left = mg - tc.m_blk * C::TILE_M - static_cast<int>(rank) * BM - lane;  // > 32 i: row lane + 32 i exists
         const float* sa = p.SA + (static_cast<long long>(row0[tc.g]) + mg - left) * p.sa_pitch;
-        // lanes 0 and 1: the two halves' column blocks (a half beyond N: the last
+        // lanes 0 and 1: the tile's two column blocks (one beyond N: the last
         // block's, its columns are not stored)
         int nb = MODE == QUANT_SWIGLU ? tc.n_blk : 2 * tc.n_blk + (lane & 1);
         if (nb >= p.n_nb) nb = p.n_nb - 1;
@@ -411,7 +411,8 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
     // the buffer in turn: its columns, its barriers (8 bytes apart, pairs aligned
     // to 16) and its phase
     uint32_t t_at = t_row, full_at = smem_u32(&tfull[0]), release_at = release0, bph = 0;
-    uint32_t slot = 0, sph = 0;  // of the scales
+    uint32_t slot = 0, sph = 0;            // of the scales
+    bool summed = false, scaled = false;  // the next block's sums, the next group's scales are there
     int cursor = 0;
     bool ok = true;
     for (int tile = tile_first; tile < n_tiles; tile += tile_step) {
@@ -436,53 +437,66 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
         }
         s_dst[lane] = make_int2(dest, __float_as_int(sc));
       }
-      float acc[2][64];
+      float acc[128];
 #pragma unroll
-      for (int i = 0; i < 128; ++i) acc[i >> 6][i & 63] = 0.0f;
-      for (int kb0 = 0; kb0 < n_kb && ok; kb0 += SG) {
-        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sfull[slot]), sph, budget, abort_flag, &g_fp8_error));
-        if (!ok) break;
-        // the group's scales to registers (of rows that do not exist: anything,
-        // their sums are not stored)
+      for (int i = 0; i < 128; ++i) acc[i] = 0.0f;
+      for (int kb0 = 0; kb0 < n_kb; kb0 += SG) {
+        if (!__all_sync(0xffffffffu, scaled)) {
+          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sfull[slot]), sph, budget, abort_flag, &g_fp8_error));
+          if (!ok) break;
+        }
+        // the group's scales (of rows that do not exist: anything, their sums are
+        // not stored)
         const float* scales = ring + slot * RING_GROUP;
         float a[SG];
         *reinterpret_cast<float4*>(a) = *reinterpret_cast<const float4*>(scales + SG * row_in_tile);
+        float2 b_next = *reinterpret_cast<const float2*>(scales + SG * BM);
 #pragma unroll
         for (int u = 0; u < SG; ++u) {
           if (kb0 + u >= n_kb) break;
-          const float2 b = *reinterpret_cast<const float2*>(scales + SG * BM + 2 * u);
-          ok = __all_sync(0xffffffffu, mbar_wait(full_at, bph, budget, abort_flag, &g_fp8_error));
-          if (!ok) break;
+          const float2 b = b_next;
+          if (!__all_sync(0xffffffffu, summed)) {
+            ok = __all_sync(0xffffffffu, mbar_wait(full_at, bph, budget, abort_flag, &g_fp8_error));
+            if (!ok) break;
+          }
           tc_fence_after();
+          // Hands the buffer back and turns to the other one, and asks for what the
+          // next block needs: the answers come while this one's sums are added.  An
+          // answered wait takes about 100 clocks, the sums of a block 256.
+          auto release = [&] {
+            tc_fence_before();
+            __syncwarp();
+            if (PAIR) mbar_arrive_remote_if(lane == 0, release_at);
+            else mbar_arrive_if(lane == 0, release_at);
+            // both have been used once more after the second
+            bph ^= (t_at / BN) & 1u;
+            t_at ^= BN;
+            full_at ^= 8u;
+            release_at ^= 8u;
+            summed = mbar_test_wait(full_at, bph);
+            if (u + 1 < SG && kb0 + u + 1 < n_kb) {
+              b_next = *reinterpret_cast<const float2*>(scales + SG * BM + 2 * (u + 1));
+            } else {
+              // the group's scales have been read (into registers: b is used below)
+              mbar_arrive_if(lane == 0, smem_u32(&sempty[slot]));
+              if (++slot == RING) {
+                slot = 0;
+                sph ^= 1u;
+              }
+              scaled = mbar_test_wait(smem_u32(&sfull[slot]), sph);
+            }
+          };
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             float r[64];
             tmem_ld64(t_at + h * HALF, r);
-            if (h == 1) {
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) {
-                if (PAIR) mbar_arrive_remote(release_at);
-                else mbar_arrive(release_at);
-              }
-              // the other buffer; both have been used once more after the second
-              bph ^= (t_at / BN) & 1u;
-              t_at ^= BN;
-              full_at ^= 8u;
-              release_at ^= 8u;
-            }
+            if (h == 1) release();
             const float f = a[u] * (h ? b.y : b.x);
 #pragma unroll
-            for (int i = 0; i < 64; ++i) acc[h][i] = fmaf(r[i], f, acc[h][i]);
+            for (int i = 0; i < 64; ++i) acc[h * 64 + i] = fmaf(r[i], f, acc[h * 64 + i]);
           }
         }
-        // the group's scales have been read
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&sempty[slot]));
-        if (++slot == RING) {
-          slot = 0;
-          sph ^= 1u;
-        }
+        if (!ok) break;
       }
       if (C::QUANT) {
         // the two warps of a lane quadrant meet at named barriers: agree first
@@ -505,9 +519,10 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
           float m = 0.0f;
 #pragma unroll
           for (int i = 0; i < 64; ++i) {
-            acc[h][i] = MODE == QUANT_SWIGLU ? silu_bf16out(acc[h][i]) * acc[1][i] : gelu_erf(acc[h][i]);
+            float& v = acc[h * 64 + i];
+            v = MODE == QUANT_SWIGLU ? silu_bf16out(v) * acc[64 + i] : gelu_erf(v);
             // columns beyond N belong to other weights: not part of the block
-            if (col0 + i < p.N) m = fmaxf(m, fabsf(acc[h][i]));
+            if (col0 + i < p.N) m = fmaxf(m, fabsf(v));
           }
           s_max[part * BM + row_in_tile] = m;
           asm volatile("bar.sync %0, 64;" ::"r"(1 + q) : "memory");
@@ -519,7 +534,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
 #pragma unroll
           for (int j = 0; j < 4; ++j)
             *reinterpret_cast<U4*>(stg + lane * 64 + ((j ^ ((lane >> 1) & 3)) * 16)) =
-                fp8_pack16(&acc[h][16 * j], f.inv);
+                fp8_pack16(&acc[h * 64 + 16 * j], f.inv);
           __syncwarp();
           uint8_t* o = static_cast<uint8_t*>(p.out) + col0;
 #pragma unroll 1
@@ -549,11 +564,11 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
           for (int j = 0; j < SEGS; ++j) {
             U4 x;
             if (MODE == STORE_F32) {
-              const float* v = &acc[(c + 4 * j) >> 6][(c + 4 * j) & 63];
+              const float* v = &acc[c + 4 * j];
               x = U4{__float_as_uint(v[0] * sc), __float_as_uint(v[1] * sc), __float_as_uint(v[2] * sc),
                      __float_as_uint(v[3] * sc)};
             } else {
-              const float* v = &acc[((c + 8 * j) >> 6) & 1][(c + 8 * j) & 63];
+              const float* v = &acc[(c + 8 * j) & 127];
               x = U4{pack_bf16x2(v[0] * sc, v[1] * sc), pack_bf16x2(v[2] * sc, v[3] * sc),
                      pack_bf16x2(v[4] * sc, v[5] * sc), pack_bf16x2(v[6] * sc, v[7] * sc)};
             }

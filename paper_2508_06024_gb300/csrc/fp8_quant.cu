@@ -50,10 +50,10 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* X, long lon
                                                             const int32_t* inv_perm, int k, uint8_t* Q, float* S) {
   pdl_trigger();
   pdl_wait();
-  const long long unit = (blockIdx.x * 256LL + threadIdx.x) / LANES;
+  const uint32_t unit = blockIdx.x * (256u / LANES) + threadIdx.x / LANES;  // below 2^31 + 32
   const int part = threadIdx.x % LANES;
-  const long long row = unit / n_kb;
-  const int kb = static_cast<int>(unit - row * n_kb);
+  const long long row = unit / static_cast<uint32_t>(n_kb);
+  const int kb = static_cast<int>(unit - static_cast<uint32_t>(row) * n_kb);
   const int col = kb * FP8_BLOCK + part * PER;
   const bool in = row < rows;
   const bool mine = in && col < cols;
