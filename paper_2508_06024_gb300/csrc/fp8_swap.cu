@@ -183,8 +183,10 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
+  // offsets and weights are inputs of the call, which its first kernel, launched
+  // without overlap, has waited for: they are read before the wait for the kernel
+  // before this one
   if (warp == 0) {
-    pdl_wait();
     scan_groups<ROWS>(p.sh, lane, row0, cnt, prefix, blockIdx.x == 0);
     if (lane == 0) {
       tma_prefetch_desc(&tmX);
@@ -201,7 +203,6 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  pdl_wait();
   const uint32_t tmem_base = *tmem_slot;
   const int n_kb = p.sh.n_kb;
   const long long total = static_cast<long long>(prefix[p.sh.G]) * p.sh.n_nb * p.sh.mats * n_kb;
@@ -223,25 +224,56 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
     int cursor = 0, tile = tile0, kb = kb_first;
     bool ok = true;
     Tile t{};
-    for (int i = 0; i < n; ++i) {
+    // block i's place, tile by tile
+    auto place = [&](int i) {
       if (i == 0 || kb == 0) t = decode_tile<ROWS>(p.sh, tile, row0, cnt, prefix, cursor);
+    };
+    auto next = [&] {
+      if (++kb == n_kb) {
+        kb = 0;
+        ++tile;
+      }
+    };
+    auto load_w = [&](int s) {
+      const uint32_t fb = smem_u32(&full[s]);
+      mbar_expect_tx(fb, C::STAGE_BYTES);
+      tma_load_2d(smem_u32(sW + s * C::W_BYTES), t.mat ? &tmW2 : &tmW, kb * BK, t.g * p.sh.N + t.nb * BM, fb);
+    };
+    auto load_x = [&](int s) {
+      tma_load_2d(smem_u32(sX + s * C::X_BYTES), &tmX, kb * BK, t.row, smem_u32(&full[s]));
+    };
+    // the first stages' weights while the kernel before ends, then their rows
+    const int pre = n < STAGES ? n : STAGES;
+    for (int i = 0; i < pre; ++i, next()) {
+      place(i);
+      if (issue) load_w(i);
+    }
+    pdl_wait();
+    cursor = 0;
+    tile = tile0;
+    kb = kb_first;
+    for (int i = 0; i < pre; ++i, next()) {
+      place(i);
+      if (issue) load_x(i);
+      issued |= 1u << i;
+    }
+    if (pre < STAGES) {
+      stage = pre;
+    } else {
+      phase = 1u;
+    }
+    for (int i = pre; i < n; ++i, next()) {
+      place(i);
       ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&empty[stage]), phase ^ 1u, budget, abort_flag, &g_fp8_swap_error));
       if (!ok) break;
-      const uint32_t fb = smem_u32(&full[stage]);
       if (issue) {
-        mbar_expect_tx(fb, C::STAGE_BYTES);
-        tma_load_2d(smem_u32(sW + stage * C::W_BYTES), t.mat ? &tmW2 : &tmW, kb * BK, t.g * p.sh.N + t.nb * BM, fb);
-        tma_load_2d(smem_u32(sX + stage * C::X_BYTES), &tmX, kb * BK, t.row, fb);
+        load_w(stage);
+        load_x(stage);
       }
-      issued |= 1u << stage;
       issued_phase = (issued_phase & ~(1u << stage)) | (phase << stage);
       if (++stage == STAGES) {
         stage = 0;
         phase ^= 1u;
-      }
-      if (++kb == n_kb) {
-        kb = 0;
-        ++tile;
       }
     }
     if (!ok || *abort_flag) {
@@ -291,6 +323,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
     }
   } else if (warp == 2) {
     // ------------------------------------------------------------------ scales
+    pdl_wait();  // the rows' scales
     const uint32_t ring_at = smem_u32(ring);
     int slot = 0;
     uint32_t sph = 0;
@@ -321,6 +354,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
     cp_async_wait();  // none in flight when shared memory is released
   } else if (warp >= FIRST_SUM) {
     // -------------------------------------------------------------------- sums
+    pdl_wait();  // the kernel before may still read the partial sums' space
     const int q = warp & 3;  // TMEM lane quadrant
     const uint32_t t_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16);
     int slot = 0, buf = 0;
