@@ -292,8 +292,9 @@ ec2moe_status ec2moe_last_device_error(ec2moe_stream_t stream);
  * return; ec2moe_last_device_error then reports EC2MOE_ERR_TIMEOUT and the
  * context stays usable.  With a budget of 0 a wait gives up when the hardware's
  * own try (which may suspend for a few microseconds) finds it unsatisfied, and
- * the fp32 GEMM's waits for its accumulators at once; that is how failure
- * handling is exercised without a real fault.  Negative values return
+ * the fp32 GEMM's waits for its accumulators and those of the 8-bit products and
+ * the gate logits for their operands at once; that is how failure handling is
+ * exercised without a real fault.  Negative values return
  * EC2MOE_ERR_INVALID_ARG. */
 ec2moe_status ec2moe_set_wait_budget(int64_t cycles);
 int64_t ec2moe_get_wait_budget(void);

@@ -309,7 +309,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
         for (int kb = 0; kb < n_kb; ++kb, ++it) {
           const uint32_t buf = it & 1u, bph = (it >> 1) & 1u;
           // the operands first: they are there while the buffer is still being read
-          const bool there = mbar_wait(smem_u32(&full[stage]), phase, budget, abort_flag, &g_fp8_error);
+          const bool there = mbar_wait_strict(smem_u32(&full[stage]), phase, budget, abort_flag, &g_fp8_error);
           if (!__all_sync(0xffffffffu,
                           there && (PAIR ? mbar_wait_cluster(smem_u32(&tempty[buf]), bph ^ 1u, budget, abort_flag, &g_fp8_error)
                                          : mbar_wait(smem_u32(&tempty[buf]), bph ^ 1u, budget, abort_flag, &g_fp8_error)))) {

@@ -291,7 +291,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
     uint32_t phase = 0, bph = 0;
     bool ok = true, any = false;
     for (int i = 0; i < n; ++i) {
-      const bool there = mbar_wait(smem_u32(&full[stage]), phase, budget, abort_flag, &g_fp8_swap_error);
+      const bool there = mbar_wait_strict(smem_u32(&full[stage]), phase, budget, abort_flag, &g_fp8_swap_error);
       ok = __all_sync(0xffffffffu, there && mbar_wait(smem_u32(&tempty[buf]), bph ^ 1u, budget, abort_flag, &g_fp8_swap_error));
       if (!ok) break;
       tc_fence_after();

@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(LG_THREADS, 1)
         // X w0, and where three terms are too wide for one MMA X w1 + X w2
         const uint32_t d0 = tmem_base + buf * 2 * ACC_COLS, d1 = d0 + ACC_COLS;
         for (int kb = seg; kb < kb1 && kb < seg + SEG; ++kb) {
-          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&full[stage]), phase, budget, abort_flag, &g_logits_error));
+          ok = __all_sync(0xffffffffu, mbar_wait_strict(smem_u32(&full[stage]), phase, budget, abort_flag, &g_logits_error));
           if (!ok) break;
           tc_fence_after();
           const uint32_t at = smem_u32(smem + stage * stage_bytes);

@@ -105,6 +105,28 @@ def test_one_segment(T, E, K, k, n_allowed, top_groups):
     check(*case(np.random.default_rng(T + E), T, E, K, k, n_allowed, top_groups), K, top_groups=top_groups)
 
 
+# Batches beyond the one-launch size, on every arrangement of the logits: lanes of 8
+# and of 4 logits, aligned to 16 bytes or not, and rows in shared memory.
+@pytest.mark.parametrize("T,E,K,k,n_allowed,top_groups", [
+    (4000, 64, 8, 6, 32, 0), (3100, 64, 8, 6, 40, 3), (9000, 8, 2, 2, 6, 0), (20001, 16, 1, 1, 12, 0), (2500, 128, 16, 8, 70, 5),
+    (5600, 12, 3, 3, 9, 0), (3500, 48, 12, 5, 30, 4), (2800, 96, 12, 6, 60, 0), (2800, 96, 1, 6, 60, 0), (9000, 16, 4, 2, 12, 2)])
+def test_long_batches(T, E, K, k, n_allowed, top_groups):
+    rng = np.random.default_rng(T)
+    seg = [0, 100, 100, T // 2 + 1, T]
+    check(*case(rng, T, E, K, k, n_allowed, top_groups), K, top_groups=top_groups, valid=rng.random(T) > 0.1, seg=seg)
+
+
+def test_many_short_segments():
+    T = 3000
+    seg = sorted(np.random.default_rng(5).integers(0, T, 900).tolist())
+    check(*case(np.random.default_rng(6), T, 64, 8, 6, 32), 8, seg=[0] + seg + [T])
+
+
+def test_rows_with_a_pitch():
+    for T in (300, 4000):
+        check(*case(np.random.default_rng(T), T, 64, 8, 6, 32), 8, ld=77)
+
+
 @pytest.mark.parametrize("seg", [[0, 700], [0, 1, 700], [0, 0, 350, 350, 699, 700, 700], [0, 100, 101, 400, 650],
                                  list(range(0, 701, 7))])
 @pytest.mark.parametrize("padded", [0.0, 0.4])
@@ -189,9 +211,10 @@ def test_ids_out_of_range_are_skipped():
     assert C.ec2moe_last_device_error() == C.OK
 
 
-@pytest.mark.parametrize("seg", [[0, 50, 20, 40], [-3, 10, 40], [0, 10, 99]])
-def test_bad_segments_are_reported(seg):
-    z, mask, idx = case(np.random.default_rng(7), 40, 8, 2, 2, 8)
+@pytest.mark.parametrize("T", [40, 9000])
+@pytest.mark.parametrize("seg", [[0, 50, 20, 40], [-3, 10, 40], [0, 10, 9999]])
+def test_bad_segments_are_reported(seg, T):
+    z, mask, idx = case(np.random.default_rng(7), T, 8, 2, 2, 8)
     loss, counts, d, _, status = run(z, mask, idx, 2, seg=seg)
     assert status == C.ERR_INVALID_ARG and np.isfinite(loss) and np.isfinite(d).all()
     assert C.ec2moe_last_device_error() == C.OK
@@ -208,7 +231,8 @@ def test_outputs_that_are_not_wanted_and_repeats():
 # ----------------------------------------------------------------- logits
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("T,d,E,K", [(1, 8, 1, 1), (1, 512, 8, 2), (5, 264, 10, 5), (130, 768, 64, 1), (257, 2048, 64, 8),
-                                     (100, 1032, 128, 16), (300, 4096, 8, 2), (64, 520, 24, 3)])
+                                     (100, 1032, 128, 16), (300, 4096, 8, 2), (64, 520, 24, 3),
+                                     (20000, 64, 8, 1), (5000, 264, 40, 5), (2000, 136, 16, 1), (400, 200, 112, 16)])
 def test_gate_logits(dtype, T, d, E, K):
     rng = np.random.default_rng(T + d)
     dt = torch.bfloat16 if dtype == "bf16" else torch.float32
@@ -227,3 +251,32 @@ def test_gate_logits(dtype, T, d, E, K):
     want, mag = x @ W.T.astype(float) + b, np.abs(x) @ np.abs(W.T.astype(float)) + np.abs(b)
     err = np.abs(out[:-1].double().cpu().numpy() - want)
     assert (err <= (32 + d / 512 + 8) * 2.0 ** -23 * mag).all(), np.max(err / mag)
+
+
+def test_gate_logits_zero_wait_budget_times_out_and_recovers():
+    T, d, E, K = 20000, 2048, 64, 8
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    X = torch.randn(T, d, generator=g, device="cuda").to(torch.bfloat16)
+    W = [torch.randn(n, d, generator=g, device="cuda") for n in (E, K)]
+    b = [torch.zeros(n, device="cuda") for n in (E, K)]
+    desc = C.make_desc(T=T, d=d, E=E, d_ff=0, k=1, n_groups=K)
+    wsb = C.ec2moe_gate_logits_workspace_size(desc)
+    ws = torch.empty(wsb, dtype=torch.uint8, device="cuda")
+
+    def call():
+        out = torch.zeros(T, E + K, device="cuda")
+        C.ec2moe_gate_logits(desc, X, W[0], b[0], W[1], b[1], out, ws, wsb)
+        return out, C.ec2moe_last_device_error()
+
+    ref, status = call()
+    assert status == C.OK
+    old = C.ec2moe_get_wait_budget()
+    try:
+        C.ec2moe_set_wait_budget(0)
+        status = call()[1]
+    finally:
+        C.ec2moe_set_wait_budget(old)
+    assert status == C.ERR_TIMEOUT
+    again, status = call()
+    assert status == C.OK and torch.equal(again, ref)

@@ -219,6 +219,60 @@ def test_nan_stays_in_its_row():
     assert torch.equal(got[keep], want[keep]) and torch.isnan(got[[3, 12]]).all()
 
 
+# Calls of several waves of whole tiles: 256-row tiles on CTA pairs, 128-row ones on
+# single CTAs; scales whose rows align to 16, 8 and 4 bytes (K = 400, 768, 272).
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,N,K,counts", [(2048, 4096, 272, None), (1000, 272, 768, None), (900, 528, 400, [512, 388]),
+                                             (1040, 4096, 400, [130] * 8), (777, 2064, 768, [300, 0, 477]),
+                                             (160, 4096, 16, None)])
+def test_product_of_many_tiles(dtype, rows, N, K, counts):
+    offsets = None if counts is None else [0] + np.cumsum(counts).tolist()
+    product_check(np.random.default_rng(rows + K), rows, N, K, offsets, dtype)
+
+
+# Few rows, many K blocks: a tile's sums come from several CTAs.
+@pytest.mark.parametrize("rows,N,K,counts", [(1, 128, 14336, None), (100, 144, 4096, None), (3, 4096, 2048, [1, 0, 2]),
+                                             (40, 1408, 2048, [0, 20, 3, 17])])
+def test_product_split_over_k(rows, N, K, counts):
+    offsets = None if counts is None else [0] + np.cumsum(counts).tolist()
+    product_check(np.random.default_rng(rows + K), rows, N, K, offsets, "fp32")
+
+
+def test_long_rows_of_offsets():
+    """128 groups, most of them empty, rows at the end of a large operand."""
+    counts = [0] * 128
+    counts[5], counts[127] = 700, 2
+    product_check(np.random.default_rng(6), 702, 128, 128, [0] + np.cumsum(counts).tolist(), "bf16")
+
+
+@pytest.mark.parametrize("rows,N,K,G", [(4096, 2048, 2048, 2), (800, 4096, 2048, 8), (8, 4096, 4096, 4)],
+                         ids=["pairs", "single", "few-rows"])
+def test_zero_wait_budget_times_out_and_recovers(rows, N, K, G):
+    rng = np.random.default_rng(rows)
+    a, sa, b, sb = operands(rng, rows, G, N, K)
+    dev = [cuda(v) for v in (a, sa)], [cuda(v) for v in (b, sb)]
+    off = cuda(np.linspace(0, rows, G + 1).astype(np.int32))
+    wsb = C.ec2moe_fp8_gemm_workspace_size(G, rows, N, K)
+    ws = torch.empty(max(16, wsb), dtype=torch.uint8, device="cuda")
+
+    def call():
+        Y = torch.zeros(rows, N, device="cuda")
+        C.ec2moe_fp8_gemm(G, rows, N, K, *dev[0], off, *dev[1], C.F32, Y, N, ws, wsb)
+        return Y, C.ec2moe_last_device_error()
+
+    ref, status = call()
+    assert status == C.OK
+    old = C.ec2moe_get_wait_budget()
+    try:
+        C.ec2moe_set_wait_budget(0)
+        status = call()[1]
+    finally:
+        C.ec2moe_set_wait_budget(old)
+    assert status == C.ERR_TIMEOUT
+    again, status = call()
+    assert status == C.OK and torch.equal(again, ref)
+
+
 # ----------------------------------------------------------------- experts
 def routed(rng, T, E, k, allowed):
     idx = np.stack([rng.permutation(allowed)[:k] for _ in range(T)]).astype(np.int64)
@@ -253,7 +307,8 @@ def experts_case(rng, T, E, k, d, ff, act, allowed):
 @pytest.mark.parametrize("T,E,k,d,ff,act,allowed", [
     (1, 4, 2, 256, 384, C.SWIGLU, [1, 3]), (1, 1, 1, 16, 16, C.GELU, [0]), (5, 8, 2, 272, 400, C.SWIGLU, [0, 2, 3, 7]),
     (16, 4, 1, 512, 1408, C.GELU, [0, 1, 2, 3]), (70, 8, 3, 400, 528, C.GELU, list(range(8))),
-    (333, 4, 2, 768, 640, C.SWIGLU, [0, 1, 3]), (1200, 3, 1, 256, 512, C.SWIGLU, [0, 1, 2])])
+    (333, 4, 2, 768, 640, C.SWIGLU, [0, 1, 3]), (1200, 3, 1, 256, 512, C.SWIGLU, [0, 1, 2]),
+    (600, 1, 1, 256, 400, C.GELU, [0]), (150, 1, 1, 144, 272, C.GELU, [0]), (40, 8, 2, 272, 1408, C.SWIGLU, [2, 5])])
 def test_experts(dtype, T, E, k, d, ff, act, allowed):
     rng = np.random.default_rng(T + d)
     perm, offsets, Q, S, dev, wide, tw = experts_case(rng, T, E, k, d, ff, act, allowed)
