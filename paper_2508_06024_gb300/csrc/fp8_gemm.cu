@@ -521,9 +521,15 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
 #pragma unroll
           for (int i = 0; i < 64; ++i) {
             float& v = acc[h * 64 + i];
-            v = MODE == QUANT_SWIGLU ? silu_bf16out(v) * acc[64 + i] : gelu_erf(v);
+            v = MODE == QUANT_SWIGLU ? silu_bf16out(v) * acc[64 + i] : gelu_fp8out(v);
+            m = fmaxf(m, fabsf(v));
+          }
+          if (col0 + 64 > p.N) {
             // columns beyond N belong to other weights: not part of the block
-            if (col0 + i < p.N) m = fmaxf(m, fabsf(v));
+            m = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 64; ++i)
+              if (col0 + i < p.N) m = fmaxf(m, fabsf(acc[h * 64 + i]));
           }
           s_max[part * BM + row_in_tile] = m;
           asm volatile("bar.sync %0, 64;" ::"r"(1 + q) : "memory");

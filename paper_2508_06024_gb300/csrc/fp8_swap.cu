@@ -479,10 +479,10 @@ __global__ void __launch_bounds__(256) fp8_swap_sum_kernel(const SumParams p) {
           v[0].z = silu_bf16out(v[0].z) * v[1].z;
           v[0].w = silu_bf16out(v[0].w) * v[1].w;
         } else {
-          v[0].x = gelu_erf(v[0].x);
-          v[0].y = gelu_erf(v[0].y);
-          v[0].z = gelu_erf(v[0].z);
-          v[0].w = gelu_erf(v[0].w);
+          v[0].x = gelu_fp8out(v[0].x);
+          v[0].y = gelu_fp8out(v[0].y);
+          v[0].z = gelu_fp8out(v[0].z);
+          v[0].w = gelu_fp8out(v[0].w);
         }
         // columns beyond N belong to other weights: not part of the block
         float m = col < p.sh.N ? fmaxf(fmaxf(fabsf(v[0].x), fabsf(v[0].y)), fmaxf(fabsf(v[0].z), fabsf(v[0].w))) : 0.0f;
