@@ -587,7 +587,8 @@ ec2moe_status check_fp8_experts(const ec2moe_layer_desc* d) {
 }
 
 cudaError_t run_fp8(const Fp8GemmArgs& g, int epi, cudaStream_t s) {
-  return fp8_swap_rows(g.G, g.rows, g.N, epi == EPI_SWIGLU ? 2 : 1) ? launch_gemm_fp8_swap(g, epi, s) : launch_gemm_fp8(g, epi, s);
+  const bool few = fp8_swap_pays(g.G, g.rows, g.N, g.K, epi == EPI_SWIGLU ? 2 : 1);
+  return few ? launch_gemm_fp8_swap(g, epi, s) : launch_gemm_fp8(g, epi, s);
 }
 
 // Workspace of ec2moe_experts_fp8: hidden rows (at 0), their scales (a row's
@@ -603,8 +604,8 @@ Fp8Ws fp8_ws(const ec2moe_layer_desc* d) {
   w.hs_pitch = ((d->d_ff + EC2MOE_FP8_BLOCK - 1) / EC2MOE_FP8_BLOCK + 3) / 4 * 4;
   w.hs = align_up(rows * d->d_ff);
   w.part = w.hs + align_up(rows * w.hs_pitch * 4);
-  const size_t up = fp8_swap_bytes(d->E, (int)rows, d->d_ff, d->act == EC2MOE_SWIGLU ? 2 : 1);
-  const size_t down = fp8_swap_bytes(d->E, (int)rows, d->d, 1);
+  const size_t up = fp8_swap_bytes(d->E, (int)rows, d->d_ff, d->d, d->act == EC2MOE_SWIGLU ? 2 : 1);
+  const size_t down = fp8_swap_bytes(d->E, (int)rows, d->d, d->d_ff, 1);
   w.total = w.part + align_up(up > down ? up : down);
   return w;
 }
@@ -1141,7 +1142,7 @@ ec2moe_status ec2moe_fp8_quantize(int32_t dtype, int32_t n_mats, int32_t rows, i
 
 size_t ec2moe_fp8_gemm_workspace_size(int32_t n_groups, int32_t rows, int32_t N, int32_t K) {
   if (check_fp8_shape(n_groups, rows, N, K) != EC2MOE_OK) return 0;
-  return align_up(fp8_swap_bytes(n_groups, rows, N, 1));
+  return align_up(fp8_swap_bytes(n_groups, rows, N, K, 1));
 }
 
 ec2moe_status ec2moe_fp8_gemm(int32_t n_groups, int32_t rows, int32_t N, int32_t K, const void* A,

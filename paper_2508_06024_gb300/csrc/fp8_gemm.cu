@@ -28,6 +28,14 @@
 // cta_group::2; each stages its own 128 rows of A and half of the B tile, and
 // reads its own 128 rows of sums.  The even CTA issues the MMAs.
 //
+// Shared K (few tiles, stored sums): with at most half as many tiles as SMs, the 2 to
+// 8 CTAs of a cluster divide a tile's K blocks.  Each leaves its sums where its
+// operand stages were; after a cluster barrier CTA r adds up the r-th share of the
+// rows, in the order of the parts, through distributed shared memory.  One group 4096
+// x 14336: 129 rows 53 us -> 25, 300 rows 57 -> 37; 4096 x 4096, 129 rows 20 -> 16.
+// Parts of less than MIN_GROUPS groups of blocks cost what they save (1024 x 1024: 14
+// us in parts of one group, 12 whole).
+//
 // Every wait is bounded as in the bf16 kernel: a wait that gives up sets the
 // error word and the CTA's abort flag, waits for copies and MMAs in flight,
 // frees its tensor memory and returns.
@@ -63,6 +71,8 @@ constexpr int NUM_THREADS = 32 * (FIRST_SUM + SUM_WARPS);
 // quantising modes spilled 130 bytes (experts, Mixtral 8192: 2451 us, now 2356).
 constexpr int REGS_FEW = 40, REGS_SUM = 232;
 constexpr int MAX_GROUPS = 136;
+constexpr int MAX_PIECES = 8;
+constexpr int MIN_GROUPS = 2;
 constexpr int TMEM_COLS = 512;
 // Scales are handed over for SG blocks of K at a time: a wait and a release cost
 // about 200 clocks, a block's MMAs 512.
@@ -83,6 +93,7 @@ struct Params {
   const int32_t* offsets;    // [G + 1], nullptr: one group of all rows
   int G, rows, N, K, n_kb, n_nb;
   int n_tiles_n;
+  int pieces;                // CTAs of a cluster that share a tile's K (1: no cluster)
   void* out;                 // STORE: [rows, ldo]; QUANT: e4m3 [rows, N]
   long long ldo;
   float* out_scale;          // QUANT: [rows, ceil(N / 128)], pitch out_scale_pitch
@@ -115,6 +126,9 @@ struct Cfg {
   static constexpr int STAGES = PAIR ? 5 : 4;
   static constexpr int OUT_COLS = MODE == QUANT_SWIGLU ? HALF : BN;  // columns of the result per tile
   static constexpr int BUFS = TMEM_COLS / BN;
+  static constexpr bool PIECES = !QUANT && !PAIR;  // a tile's K can be shared by a cluster
+  static constexpr int SUM_PITCH = BN + 4;         // floats of a row of the sums handed over
+  static_assert(BM * SUM_PITCH * 4 <= STAGES * STAGE_BYTES || !PIECES, "the sums take the place of the stages");
   static constexpr int N_BARS = 2 * STAGES + 2 * BUFS + 2 * RING + 1;  // full, empty, tfull, tempty, sfull, sempty, drain
   static constexpr int OFF_BARS = STAGES * STAGE_BYTES;
   static constexpr int OFF_SLOT = OFF_BARS + N_BARS * 8;
@@ -160,8 +174,12 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
   const uint32_t rank = PAIR ? cluster_ctarank() : 0u;
-  const int tile_first = PAIR ? static_cast<int>(cluster_id_x()) : static_cast<int>(blockIdx.x);
-  const int tile_step = PAIR ? static_cast<int>(cluster_count_x()) : static_cast<int>(gridDim.x);
+  const bool shared_k = C::PIECES && p.pieces > 1;  // the cluster has one tile, or none
+  const int tile_first = PAIR || shared_k ? static_cast<int>(cluster_id_x()) : static_cast<int>(blockIdx.x);
+  const int tile_step = PAIR       ? static_cast<int>(cluster_count_x())
+                        : shared_k ? 1 << 30
+                                   : static_cast<int>(gridDim.x);
+  const int piece = shared_k ? static_cast<int>(cluster_ctarank()) : 0;
   // Barrier set-up, TMEM allocation and descriptor prefetch overlap the previous
   // kernel; everything that reads its results comes after pdl_wait.
   pdl_trigger();
@@ -232,7 +250,10 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
   pdl_wait();
   const uint32_t tmem_base = *tmem_slot;
   const int n_tiles = tile_prefix[p.G] * p.n_tiles_n;
-  const int n_kb = p.n_kb;
+  // this CTA's blocks of K: all, or its share in whole groups of SG
+  const int n_sg = (p.n_kb + SG - 1) / SG;
+  const int kb_first = shared_k ? piece * n_sg / p.pieces * SG : 0;
+  const int n_kb = (shared_k && piece + 1 < p.pieces ? (piece + 1) * n_sg / p.pieces * SG : p.n_kb) - kb_first;
   const long long budget = p.timeout;
 
   if (warp < FIRST_SUM) {
@@ -259,20 +280,21 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
           const uint32_t fb = smem_u32(&full[stage]);
           const uint32_t da = smem_u32(sA + stage * C::A_BYTES);
           const uint32_t db = smem_u32(sB + stage * C::B_BYTES);
+          const int k = (kb_first + kb) * BK;
           if (!issue) {
           } else if (PAIR) {
             // both halves complete on the even CTA's full barrier; of the B tile
             // the even CTA stages the first half of the columns, the odd CTA the second
             if (rank == 0) mbar_expect_tx(fb, 2 * C::STAGE_BYTES);
             const uint32_t fb0 = rank == 0 ? fb : map_to_rank(fb, 0);
-            tma_load_2d_to_pair_bar(da, &tmA, kb * BK, a_row, fb0);
-            tma_load_2d_to_pair_bar(db, MODE == QUANT_SWIGLU && rank ? &tmB2 : &tmB, kb * BK,
+            tma_load_2d_to_pair_bar(da, &tmA, k, a_row, fb0);
+            tma_load_2d_to_pair_bar(db, MODE == QUANT_SWIGLU && rank ? &tmB2 : &tmB, k,
                                     b_row + (MODE == QUANT_SWIGLU ? 0 : static_cast<int>(rank) * HALF), fb0);
           } else {
             mbar_expect_tx(fb, C::STAGE_BYTES);
-            tma_load_2d(da, &tmA, kb * BK, a_row, fb);
-            tma_load_2d(db, &tmB, kb * BK, b_row, fb);
-            tma_load_2d(db + HALF * BK, MODE == QUANT_SWIGLU ? &tmB2 : &tmB, kb * BK,
+            tma_load_2d(da, &tmA, k, a_row, fb);
+            tma_load_2d(db, &tmB, k, b_row, fb);
+            tma_load_2d(db + HALF * BK, MODE == QUANT_SWIGLU ? &tmB2 : &tmB, k,
                         b_row + (MODE == QUANT_SWIGLU ? 0 : HALF), fb);
           }
           issued |= 1u << stage;
@@ -365,13 +387,14 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
         const TileCoord tc = decode_tile(tile, tile_prefix, p.n_tiles_n, cursor);
         const int mg = row_cnt[tc.g];
         const int left = mg - tc.m_blk * C::TILE_M - static_cast<int>(rank) * BM - lane;  // > 32 i: row lane + 32 i exists
-        const float* sa = p.SA + (static_cast<long long>(row0[tc.g]) + mg - left) * p.sa_pitch;
+        const float* sa = p.SA + (static_cast<long long>(row0[tc.g]) + mg - left) * p.sa_pitch + kb_first;
         // lanes 0 and 1: the tile's two column blocks (one beyond N: the last
         // block's, its columns are not stored)
         int nb = MODE == QUANT_SWIGLU ? tc.n_blk : 2 * tc.n_blk + (lane & 1);
         if (nb >= p.n_nb) nb = p.n_nb - 1;
         const float* sb =
-            (MODE == QUANT_SWIGLU && (lane & 1) ? p.SB2 : p.SB) + (static_cast<long long>(tc.g) * p.n_nb + nb) * n_kb;
+            (MODE == QUANT_SWIGLU && (lane & 1) ? p.SB2 : p.SB) + (static_cast<long long>(tc.g) * p.n_nb + nb) * p.n_kb +
+            kb_first;
         for (int kb0 = 0; kb0 < n_kb; kb0 += SG, ++it) {
           const uint32_t slot = it % RING, sph = (it / RING) & 1u;
           ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sempty[slot]), sph ^ 1u, budget, abort_flag, &g_fp8_error));
@@ -398,6 +421,10 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
         }
       }
       cp_async_wait();  // none in flight when shared memory is released
+    }
+    if (shared_k) {
+      __syncwarp();
+      cluster_sync_all();
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SUM));
@@ -555,6 +582,12 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
           // the other warp has read this half's magnitudes before they change
           asm volatile("bar.sync %0, 64;" ::"r"(1 + q) : "memory");
         }
+      } else if (shared_k) {
+        // handed over where the operands were, which have all been multiplied
+        float* to = reinterpret_cast<float*>(smem) + row_in_tile * C::SUM_PITCH + part * 64;
+#pragma unroll
+        for (int i = 0; i < 128; i += 4)
+          *reinterpret_cast<float4*>(to + (i >> 6) * HALF + (i & 63)) = make_float4(acc[i], acc[i + 1], acc[i + 2], acc[i + 3]);
       } else {
         // Slabs of SLAB columns: rounded into the warp's staging rows (16-byte
         // chunks XOR-swizzled by row), then stored as whole row segments.  The
@@ -595,13 +628,55 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
         __syncwarp();
       }
     }
+    if (shared_k) {
+      // CTA r of the cluster adds and stores rows [r BM / pieces, (r + 1) BM / pieces)
+      // of the tile, the pieces in their order.
+      __syncwarp();
+      cluster_sync_all();
+      if (tile_first < n_tiles) {
+        int from = 0;
+        const TileCoord tc = decode_tile(tile_first, tile_prefix, p.n_tiles_n, from);
+        const int2* dst = reinterpret_cast<const int2*>(smem + C::OFF_DST);  // by row: its quadrant's first warp's
+        const int row_first = piece * BM / p.pieces, rows = (piece + 1) * BM / p.pieces - row_first;
+        const uint32_t sums = smem_u32(smem);
+#pragma unroll 1
+        for (int i = threadIdx.x - 32 * FIRST_SUM; i < rows * (BN / 4); i += 32 * SUM_WARPS) {
+          const int r = row_first + i / (BN / 4), c = i % (BN / 4) * 4;
+          const int2 to = dst[r];
+          const int col = tc.n_blk * BN + c;
+          if (to.x < 0 || col >= p.N) continue;
+          const uint32_t at = sums + (r * C::SUM_PITCH + c) * 4;
+          float4 part_of[MAX_PIECES];
+#pragma unroll
+          for (int k = 0; k < MAX_PIECES; ++k)
+            if (k < p.pieces) part_of[k] = ld_cluster_v4(map_to_rank(at, k));
+          float4 v = part_of[0];
+#pragma unroll
+          for (int k = 1; k < MAX_PIECES; ++k) {
+            if (k >= p.pieces) break;
+            v.x += part_of[k].x;
+            v.y += part_of[k].y;
+            v.z += part_of[k].z;
+            v.w += part_of[k].w;
+          }
+          const float sc = __int_as_float(to.y);
+          const long long o = to.x * p.ldo + col;
+          if (MODE == STORE_F32)
+            *reinterpret_cast<float4*>(static_cast<float*>(p.out) + o) = make_float4(v.x * sc, v.y * sc, v.z * sc, v.w * sc);
+          else
+            *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + o) =
+                make_uint2(pack_bf16x2(v.x * sc, v.y * sc), pack_bf16x2(v.z * sc, v.w * sc));
+        }
+      }
+    }
   }
 
   tc_fence_before();
   __syncthreads();
   // PAIR: the even CTA's MMAs write both CTAs' TMEM; neither releases its
-  // columns before both are done with them
-  if (PAIR) cluster_sync_all();
+  // columns before both are done with them.  Shared K: no CTA ends while its sums
+  // are read.
+  if (PAIR || shared_k) cluster_sync_all();
   if (warp == 1) {
     tc_fence_after();
     if (PAIR)
@@ -614,6 +689,22 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
 }
 
 // ------------------------------------------------------------------ host side
+// Tiles of a call at most: every group that has rows may end inside one.
+long long max_tiles(const Fp8GemmArgs& a, int tile_m, int out_cols) {
+  const long long live = a.rows < a.G ? a.rows : a.G;
+  return (a.rows + live * (tile_m - 1)) / tile_m * ((a.N + out_cols - 1) / out_cols);
+}
+
+// Among how many CTAs a tile's K is divided: as many as give every cluster a place
+// at once, and each CTA MIN_GROUPS groups of SG blocks.
+int k_pieces(const void* kfn, int smem, long long tiles, int n_kb) {
+  long long n = tiles > 0 ? sm_count() / tiles : 1;
+  if (n > MAX_PIECES) n = MAX_PIECES;
+  if (n > n_kb / (MIN_GROUPS * SG)) n = n_kb / (MIN_GROUPS * SG);
+  while (n > 1 && tiles > max_clusters(kfn, NUM_THREADS, smem, static_cast<int>(n))) --n;
+  return n > 1 ? static_cast<int>(n) : 1;
+}
+
 template <int MODE, bool PAIR>
 cudaError_t launch_cfg(const Fp8GemmArgs& a, cudaStream_t s) {
   using C = Cfg<MODE, PAIR>;
@@ -649,13 +740,18 @@ cudaError_t launch_cfg(const Fp8GemmArgs& a, cudaStream_t s) {
   p.perm = a.perm;
   p.row_scale = a.row_scale;
   p.timeout = a.timeout_cycles;
-  const long long tiles = (static_cast<long long>(a.rows) / C::TILE_M + a.G) * p.n_tiles_n;
+  p.pieces = 1;
+  const long long tiles = max_tiles(a, C::TILE_M, C::OUT_COLS);
   KernelScope ks(a.name, s);
   if (PAIR) {
     int clusters = max_clusters(kfn, NUM_THREADS, C::SMEM, 2);
     if (clusters < 1) return cudaErrorInvalidConfiguration;
     if (tiles < clusters) clusters = static_cast<int>(tiles);
     e = launch_cluster(fp8_gemm_kernel<MODE, PAIR>, clusters, 2, NUM_THREADS, (size_t)C::SMEM, s, mA, mB, mB2, p);
+  } else if (int pieces = C::PIECES ? k_pieces(kfn, C::SMEM, tiles, p.n_kb) : 1; pieces > 1) {
+    p.pieces = pieces;
+    e = launch_cluster(fp8_gemm_kernel<MODE, PAIR>, static_cast<int>(tiles), pieces, NUM_THREADS, (size_t)C::SMEM, s, mA,
+                       mB, mB2, p);
   } else {
     const int grid = static_cast<int>(tiles < sm_count() ? tiles : sm_count());
     e = launch_kernel(fp8_gemm_kernel<MODE, PAIR>, dim3(grid), dim3(NUM_THREADS), (size_t)C::SMEM, s, mA, mB, mB2, p);
@@ -664,18 +760,25 @@ cudaError_t launch_cfg(const Fp8GemmArgs& a, cudaStream_t s) {
   return cudaGetLastError();
 }
 
-// 256-row tiles on CTA pairs where the expected rows per group waste at most a
-// tenth more rows in them than in 128-row tiles.
+// 256-row tiles on CTA pairs where they waste at most a tenth more rows than 128-row
+// tiles.  Several groups end inside a tile each, on average half of one, however
+// even their expected rows: six experts of 341 rows where 256 were expected took 455
+// us in pairs, 367 in single tiles.  Not where clusters can share K instead.
+template <int MODE>
 bool use_pairs(const Fp8GemmArgs& a) {
-  const long long per = a.rows / (a.g_active > 0 ? a.g_active : a.G);
-  if (per < 2 * BM) return false;
-  const long long pad1 = (per + BM - 1) / BM * BM, pad2 = (per + 2 * BM - 1) / (2 * BM) * (2 * BM);
+  using C = Cfg<MODE, false>;
+  if (C::PIECES && 2 * max_tiles(a, C::TILE_M, C::OUT_COLS) <= sm_count()) return false;
+  if (a.G > 1) {
+    const long long per = a.rows / a.G;
+    return 10 * (per + BM) <= 11 * (per + BM / 2);
+  }
+  const long long pad1 = (a.rows + BM - 1) / BM * BM, pad2 = (a.rows + 2 * BM - 1) / (2 * BM) * (2 * BM);
   return 10 * pad2 <= 11 * pad1;
 }
 
 template <int MODE>
 cudaError_t launch_mode(const Fp8GemmArgs& a, cudaStream_t s) {
-  return use_pairs(a) ? launch_cfg<MODE, true>(a, s) : launch_cfg<MODE, false>(a, s);
+  return use_pairs<MODE>(a) ? launch_cfg<MODE, true>(a, s) : launch_cfg<MODE, false>(a, s);
 }
 
 }  // namespace

@@ -36,6 +36,7 @@ namespace {
 using namespace tc;
 
 constexpr int BM = 128;        // weight rows per tile
+constexpr int ROWS = 16;       // rows of the group per tile
 constexpr int BK = FP8_BLOCK;
 constexpr int UK = 32;
 constexpr int NUM_THREADS = 256;
@@ -61,7 +62,6 @@ struct Params {
 };
 
 // First rows, row counts and token-tile prefix of the groups (one warp).
-template <int ROWS>
 __device__ __forceinline__ void scan_groups(const Shape& s, int lane, int* row0, int* cnt, int* prefix, bool report) {
   warp_exclusive_scan<(MAX_GROUPS + 31) / 32>(
       s.G, lane,
@@ -88,7 +88,6 @@ struct Tile {
   int g, nb, mat;
   int row, n;  // first row and rows of the token tile
 };
-template <int ROWS>
 __device__ __forceinline__ Tile decode_tile(const Shape& s, int t, const int* row0, const int* cnt, const int* prefix,
                                             int& cursor) {
   const int per = s.n_nb * s.mats;
@@ -108,12 +107,11 @@ __device__ __forceinline__ int piece_of(long long total, long long x, int ctas) 
   return static_cast<int>(((x + 1) * ctas - 1) / total);
 }
 
-template <int ROWS>
 struct Cfg {
   static constexpr int W_BYTES = BM * BK;
   static constexpr int X_BYTES = ROWS * BK;
   static constexpr int STAGE_BYTES = W_BYTES + X_BYTES;
-  static constexpr int STAGES = ROWS == 16 ? 10 : 9;
+  static constexpr int STAGES = 10;
   static constexpr int BUFS = 8;
   static constexpr int TMEM_COLS = BUFS * ROWS;
   static constexpr int RING = 4;
@@ -132,18 +130,10 @@ struct Cfg {
   static_assert((TMEM_COLS & (TMEM_COLS - 1)) == 0 && TMEM_COLS >= 32 && TMEM_COLS <= 512, "TMEM columns");
 };
 
-// ROWS columns of fp32 TMEM words, complete on return.
-template <int ROWS>
-__device__ __forceinline__ void tmem_ld_rows(uint32_t taddr, float* v) {
-  if constexpr (ROWS == 16) tmem_ld16(taddr, v);
-  else tmem_ld32(taddr, v);
-}
-
-template <int ROWS>
 __global__ void __launch_bounds__(NUM_THREADS, 1)
     fp8_swap_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW,
                     const __grid_constant__ CUtensorMap tmW2, const Params p) {
-  using C = Cfg<ROWS>;
+  using C = Cfg;
   constexpr int STAGES = C::STAGES, BUFS = C::BUFS, RING = C::RING;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -187,7 +177,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
   // without overlap, has waited for: they are read before the wait for the kernel
   // before this one
   if (warp == 0) {
-    scan_groups<ROWS>(p.sh, lane, row0, cnt, prefix, blockIdx.x == 0);
+    scan_groups(p.sh, lane, row0, cnt, prefix, blockIdx.x == 0);
     if (lane == 0) {
       tma_prefetch_desc(&tmX);
       tma_prefetch_desc(&tmW);
@@ -226,7 +216,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
     Tile t{};
     // block i's place, tile by tile
     auto place = [&](int i) {
-      if (i == 0 || kb == 0) t = decode_tile<ROWS>(p.sh, tile, row0, cnt, prefix, cursor);
+      if (i == 0 || kb == 0) t = decode_tile(p.sh, tile, row0, cnt, prefix, cursor);
     };
     auto next = [&] {
       if (++kb == n_kb) {
@@ -334,7 +324,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
       ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sempty[slot]), sph ^ 1u, budget, abort_flag, &g_fp8_swap_error));
       if (!ok) break;
       for (int u = 0; u < SG && i + u < n; ++u) {
-        if (i + u == 0 || kb == 0) t = decode_tile<ROWS>(p.sh, tile, row0, cnt, prefix, cursor);
+        if (i + u == 0 || kb == 0) t = decode_tile(p.sh, tile, row0, cnt, prefix, cursor);
         const uint32_t to = ring_at + 4 * (slot * C::RING_GROUP + u * C::RING_ROW);
         for (int r = lane; r < t.n; r += 32)
           cp_async<4>(to + 4 * r, p.SA + static_cast<long long>(t.row + r) * p.sa_pitch + kb);
@@ -371,7 +361,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
       if (!__all_sync(0xffffffffu, ok)) break;
       tc_fence_after();
       float r[ROWS];
-      tmem_ld_rows<ROWS>(t_row + buf * ROWS, r);
+      tmem_ld16(t_row + buf * ROWS, r);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&tempty[buf]));
@@ -400,7 +390,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
       }
       if (++kb == n_kb || i == n - 1) {
         // this CTA's part of the tile
-        const Tile t = decode_tile<ROWS>(p.sh, tile, row0, cnt, prefix, cursor);
+        const Tile t = decode_tile(p.sh, tile, row0, cnt, prefix, cursor);
         float* to = p.part + (static_cast<long long>(blockIdx.x) + tile) * (ROWS * BM) + q * 32 + lane;
 #pragma unroll
         for (int j = 0; j < ROWS; ++j) {
@@ -438,21 +428,21 @@ struct SumParams {
 
 // A warp takes one token's 128 columns of a tile (of two tiles for SwiGLU), four
 // per lane; a CTA the tokens of one tile.
-template <int ROWS, int MODE>
+template <int MODE>
 __global__ void __launch_bounds__(256) fp8_swap_sum_kernel(const SumParams p) {
   __shared__ int row0[MAX_GROUPS], cnt[MAX_GROUPS], prefix[MAX_GROUPS + 1];
   constexpr bool QUANT = MODE == QUANT_GELU || MODE == QUANT_SWIGLU;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_trigger();
   pdl_wait();
-  if (warp == 0) scan_groups<ROWS>(p.sh, lane, row0, cnt, prefix, false);
+  if (warp == 0) scan_groups(p.sh, lane, row0, cnt, prefix, false);
   __syncthreads();
   const int tiles = prefix[p.sh.G] * p.sh.n_nb * p.sh.mats;
   const long long total = static_cast<long long>(tiles) * p.sh.n_kb;
   const int ctas = pieces(total, p.ctas);
   int cursor = 0;
   for (int tile = blockIdx.x * p.sh.mats; tile < tiles; tile += gridDim.x * p.sh.mats) {
-    const Tile t = decode_tile<ROWS>(p.sh, tile, row0, cnt, prefix, cursor);
+    const Tile t = decode_tile(p.sh, tile, row0, cnt, prefix, cursor);
     const int col = t.nb * BM + 4 * lane;
     for (int j = warp; j < t.n; j += 8) {
       float4 v[2];
@@ -518,12 +508,13 @@ __global__ void __launch_bounds__(256) fp8_swap_sum_kernel(const SumParams p) {
 
 // ------------------------------------------------------------------ host side
 // Token tiles that the groups can hold at most.
-long long token_tiles(int G, int rows, int per) { return (rows < G ? rows : G) + static_cast<long long>(rows) / per; }
+long long token_tiles(int G, int rows) { return (rows < G ? rows : G) + rows / ROWS; }
 
-template <int ROWS>
-cudaError_t launch_rows(const Fp8GemmArgs& a, int epi, cudaStream_t s) {
-  using C = Cfg<ROWS>;
-  const void* kfn = reinterpret_cast<const void*>(fp8_swap_kernel<ROWS>);
+}  // namespace
+
+cudaError_t launch_gemm_fp8_swap(const Fp8GemmArgs& a, int epi, cudaStream_t s) {
+  using C = Cfg;
+  const void* kfn = reinterpret_cast<const void*>(fp8_swap_kernel);
   cudaError_t e = ensure_smem_attr(kfn, C::SMEM);
   if (e != cudaSuccess) return e;
   const int mats = epi == EPI_SWIGLU ? 2 : 1;
@@ -541,11 +532,11 @@ cudaError_t launch_rows(const Fp8GemmArgs& a, int epi, cudaStream_t s) {
   p.SB2 = a.SB2;
   p.part = static_cast<float*>(a.part);
   p.timeout = a.timeout_cycles;
-  const long long tiles = token_tiles(a.G, a.rows, ROWS) * p.sh.n_nb * mats;
+  const long long tiles = token_tiles(a.G, a.rows) * p.sh.n_nb * mats;
   const int ctas = fp8_swap_ctas();
   {
     KernelScope ks(a.name, s);
-    e = launch_kernel(fp8_swap_kernel<ROWS>, dim3(ctas), dim3(NUM_THREADS), (size_t)C::SMEM, s, mX, mW, mW2, p);
+    e = launch_kernel(fp8_swap_kernel, dim3(ctas), dim3(NUM_THREADS), (size_t)C::SMEM, s, mX, mW, mW2, p);
     if (e != cudaSuccess) return e;
   }
   SumParams r;
@@ -561,48 +552,39 @@ cudaError_t launch_rows(const Fp8GemmArgs& a, int epi, cudaStream_t s) {
   const long long blocks = tiles / mats;
   const dim3 grid(static_cast<unsigned>(blocks < 4096 ? blocks : 4096));
   KernelScope ks("fp8_sum", s);
-  if (epi == EPI_SWIGLU) e = launch_kernel(fp8_swap_sum_kernel<ROWS, QUANT_SWIGLU>, grid, dim3(256), 0, s, r);
-  else if (epi == EPI_GELU) e = launch_kernel(fp8_swap_sum_kernel<ROWS, QUANT_GELU>, grid, dim3(256), 0, s, r);
-  else if (a.out_bf16) e = launch_kernel(fp8_swap_sum_kernel<ROWS, STORE_BF16>, grid, dim3(256), 0, s, r);
-  else e = launch_kernel(fp8_swap_sum_kernel<ROWS, STORE_F32>, grid, dim3(256), 0, s, r);
+  if (epi == EPI_SWIGLU) e = launch_kernel(fp8_swap_sum_kernel<QUANT_SWIGLU>, grid, dim3(256), 0, s, r);
+  else if (epi == EPI_GELU) e = launch_kernel(fp8_swap_sum_kernel<QUANT_GELU>, grid, dim3(256), 0, s, r);
+  else if (a.out_bf16) e = launch_kernel(fp8_swap_sum_kernel<STORE_BF16>, grid, dim3(256), 0, s, r);
+  else e = launch_kernel(fp8_swap_sum_kernel<STORE_F32>, grid, dim3(256), 0, s, r);
   if (e != cudaSuccess) return e;
   return cudaGetLastError();
 }
 
-}  // namespace
-
 int fp8_swap_ctas() { return sm_count(); }
 
 // The tall kernel's tiles of a call (128 rows, 256 columns of B) are whole units of
-// work: with fewer of them than SMs, or few waves, SMs are left without one, which
-// the line of blocks here is not.  It pays for that with partial sums and, beyond
-// one token tile per group, with reading the weights again.  Measured (us, this /
-// tall, cold L2): 8 groups 14336 x 4096: 2 rows 36 / 40, 8 rows 82 / 86, 32 rows 98 /
-// 94, 128 rows 101 / 96; 4096 x 14336: 2 rows 36 / 60, 32 rows 98 / 96; 64 groups 1408
-// x 2048: 48 rows 36 / 39, 192 rows 52 / 53, 768 rows 56 / 53; one group 4096 x 4096: 1
-// row 15 / 23, 64 rows 19 / 25, 128 rows 24 / 25, 256 rows 30 / 25.
-int fp8_swap_rows(int G, int rows, int N, int mats) {
+// work: with few waves of them SMs are left without one, which the line of blocks
+// here is not.  It pays for that with partial sums and, beyond one token tile per
+// group, with reading the weights again.  Measured (us, this / tall, cold L2):
+// - one wave of tiles or less: 1 group 4096 x 14336, 1 row 16 / 19, 17 rows 20 / 18,
+//   128 rows 41 / 21; 8 groups 4096 x 4096, 17 rows each 34 / 31, 65 each 53 / 31;
+// - 1.5 waves: 4 groups 14336 x 4096, 1 row each 37 / 49, 4 each 47 / 61, 8 each 48 / 48;
+// - 3 waves: 8 groups 14336 x 4096, 1 row each 65 / 76, 4 each 82 / 80; 4.6 waves of
+//   short K: 64 groups 1408 x 2048, 1 row each 30 / 29, 4 each 44 / 41.
+bool fp8_swap_pays(int G, int rows, int N, int K, int mats) {
+  if (rows == 0) return false;
   const long long groups = rows < G ? rows : G;
   const long long per = rows / groups;
   const long long tall = groups * ((static_cast<long long>(N) * mats + 255) / 256);
   const long long sms = sm_count();
-  if (tall <= sms ? per <= 128 : (2 * tall <= 5 * sms && per <= 8)) return per <= 16 ? 16 : 32;
-  return 0;
+  if (tall <= sms) return per <= 16;
+  return (2 * tall <= 5 * sms && per <= 8) || (K >= 4096 && per <= 2);
 }
 
-size_t fp8_swap_bytes(int G, int rows, int N, int mats) {
-  const int per = rows > 0 ? fp8_swap_rows(G, rows, N, mats) : 0;
-  if (per == 0) return 0;
-  const long long tiles = token_tiles(G, rows, per) * ((N + BM - 1) / BM) * mats;
-  return static_cast<size_t>(tiles + fp8_swap_ctas()) * per * BM * 4;
-}
-
-cudaError_t launch_gemm_fp8_swap(const Fp8GemmArgs& a, int epi, cudaStream_t s) {
-  switch (fp8_swap_rows(a.G, a.rows, a.N, epi == EPI_SWIGLU ? 2 : 1)) {
-    case 16: return launch_rows<16>(a, epi, s);
-    case 32: return launch_rows<32>(a, epi, s);
-  }
-  return cudaErrorInvalidValue;
+size_t fp8_swap_bytes(int G, int rows, int N, int K, int mats) {
+  if (!fp8_swap_pays(G, rows, N, K, mats)) return 0;
+  const long long tiles = token_tiles(G, rows) * ((N + BM - 1) / BM) * mats;
+  return static_cast<size_t>(tiles + fp8_swap_ctas()) * ROWS * BM * 4;
 }
 
 cudaError_t read_fp8_swap_error(unsigned int* word) {

@@ -306,17 +306,16 @@ struct Fp8GemmArgs {
   int out_scale_pitch;  // floats per row of out_scale
   const int32_t* perm;
   const float* row_scale;
-  int g_active;         // groups expected to hold rows (0 = G)
   void* part;           // launch_gemm_fp8_swap: fp8_swap_bytes() of workspace, 16-byte aligned
   long long timeout_cycles;
   const char* name;
 };
-// Groups of few rows: rows of a token tile of the swapped-operand kernel, 0 where
-// the tall kernel (launch_gemm_fp8) is the better one; the workspace of its
-// partial sums (mats: 2 for SwiGLU), whose size depends on the device's SM count.
-int fp8_swap_rows(int G, int rows, int N, int mats);
+// Groups of few rows: whether the swapped-operand kernel is the better one (else the
+// tall kernel, launch_gemm_fp8); the workspace of its partial sums (mats: 2 for
+// SwiGLU), whose size depends on the device's SM count.
+bool fp8_swap_pays(int G, int rows, int N, int K, int mats);
 int fp8_swap_ctas();
-size_t fp8_swap_bytes(int G, int rows, int N, int mats);
+size_t fp8_swap_bytes(int G, int rows, int N, int K, int mats);
 cudaError_t launch_gemm_fp8_swap(const Fp8GemmArgs& a, int epi, cudaStream_t s);
 cudaError_t read_fp8_swap_error(unsigned int* word);
 cudaError_t launch_gemm_fp8(const Fp8GemmArgs& a, int epi, cudaStream_t s);

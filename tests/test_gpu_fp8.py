@@ -273,6 +273,51 @@ def test_zero_wait_budget_times_out_and_recovers(rows, N, K, G):
     assert status == C.OK and torch.equal(again, ref)
 
 
+# Fewer tiles than half the SMs: the CTAs of a cluster (2 to 8) share a tile's K, in
+# equal and unequal parts; rows and columns end inside the tile.
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,N,K,counts", [
+    (129, 4096, 4096, None), (300, 1024, 2064, None), (50, 144, 14336, None), (257, 768, 5136, None), (17, 272, 6160, None),
+    (18, 16, 7184, None), (128, 5120, 3088, None), (278, 400, 2048, [200, 0, 1, 77]), (250, 528, 4112, [0, 249, 1])])
+def test_product_of_clusters_that_share_k(dtype, rows, N, K, counts):
+    offsets = None if counts is None else [0] + np.cumsum(counts).tolist()
+    product_check(np.random.default_rng(rows + K), rows, N, K, offsets, dtype, ldc=N + 48)
+
+
+def test_shared_k_gives_the_same_bits_again():
+    rng = np.random.default_rng(8)
+    a, sa, b, sb = (cuda(v) for v in operands(rng, 200, 1, 528, 4112))
+    Y = [torch.empty(200, 528, device="cuda") for _ in range(4)]
+    for y in Y:
+        C.ec2moe_fp8_gemm(1, 200, 528, 4112, a, sa, None, b, sb, C.F32, y, 528, None, 0)
+    assert all(torch.equal(y, Y[0]) for y in Y)
+
+
+def test_shared_k_skips_bad_groups_and_times_out():
+    rng = np.random.default_rng(9)
+    a, sa, b, sb = (cuda(v) for v in operands(rng, 300, 2, 400, 4096))
+
+    def call(offsets, rows=300):
+        Y = torch.full((304, 400), 3.0, dtype=torch.bfloat16, device="cuda")
+        C.ec2moe_fp8_gemm(2, rows, 400, 4096, a, sa, cuda(np.array(offsets, np.int32)), b, sb, C.BF16, Y, 400, None, 0)
+        return Y, C.ec2moe_last_device_error()
+
+    ref, status = call([0, 120, 300])
+    assert status == C.OK
+    for bad in ([0, 400, 300], [0, -5, 24], [200, 2, 300], [0, 300, 200]):
+        Y, status = call(bad)
+        assert status == C.ERR_INVALID_ARG and (Y[300:] == 3.0).all()
+    old = C.ec2moe_get_wait_budget()
+    try:
+        C.ec2moe_set_wait_budget(0)
+        status = call([0, 120, 300])[1]
+    finally:
+        C.ec2moe_set_wait_budget(old)
+    assert status == C.ERR_TIMEOUT
+    again, status = call([0, 120, 300])
+    assert status == C.OK and torch.equal(again, ref)
+
+
 # ----------------------------------------------------------------- experts
 def routed(rng, T, E, k, allowed):
     idx = np.stack([rng.permutation(allowed)[:k] for _ in range(T)]).astype(np.int64)
@@ -322,6 +367,15 @@ def test_experts(dtype, T, E, k, d, ff, act, allowed):
     want = orc.experts(wide["x"], offsets, wide["W1"], wide["W3"], wide["W2"], tw, perm)
     err = rel_fro(out[:-1].double().cpu().numpy(), want)
     assert err <= 3.6e-3 + (2.0 ** -9 if dtype == "bf16" else 0.0), err
+
+
+# The products back from the hidden width by clusters that share it, scattered and
+# scaled by row.
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,E,k,d,ff,act,allowed", [
+    (100, 2, 1, 272, 2064, C.GELU, [0, 1]), (70, 4, 2, 144, 5136, C.SWIGLU, [0, 1, 3]), (150, 1, 1, 512, 3600, C.GELU, [0])])
+def test_experts_share_the_hidden_width(dtype, T, E, k, d, ff, act, allowed):
+    test_experts(dtype, T, E, k, d, ff, act, allowed)
 
 
 @pytest.mark.parametrize("T", [6, 200])
