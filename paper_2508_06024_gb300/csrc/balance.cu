@@ -31,6 +31,8 @@
 // gradients; balance_final, the CTAs' partial sums in order.  Bounded by HBM for
 // long batches (the logits are read once, their gradients written once), by the
 // launches for short ones.
+#include <algorithm>
+
 #include <cuda_runtime.h>
 
 #include "common.cuh"
@@ -72,6 +74,7 @@ struct Params {
   int32_t* n_live;    // segments that hold one
   double* partial;    // [grid][O + 1]: sums of the gradients, then the loss
   int n_part;
+  int lane_steps;     // of a warp of balance_lanes
   int pitch;          // floats per token in shared memory
 };
 
@@ -93,6 +96,20 @@ __device__ __forceinline__ int segment_of(const Params& p, int t) { return segme
 __device__ __forceinline__ int segment_between(const Params& p, int t, int lo, int hi) {
   if (lo < 0 || hi < lo) return segment_of(p, t);
   return lo == hi ? lo : segment_in(p, t, lo, hi + 1);
+}
+
+// segment_of one token for a warp that asks together: 32 offsets at a time.
+__device__ __forceinline__ int segment_by_warp(const Params& p, int t, int lane) {
+  if (!p.seg_offsets) return 0;
+  int lo = 0, hi = p.n_seg;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 31) / 32, i = lo + lane * step;
+    const uint32_t before = __ballot_sync(0xffffffffu, i < hi && p.seg_offsets[i] <= t);
+    const int n = before == 0xffffffffu ? 32 : __ffs(~before) - 1;
+    if (n > 0) lo += (n - 1) * step;
+    hi = n > 0 ? min(hi, lo + step) : lo + 1;
+  }
+  return p.seg_offsets[lo] <= t && t < p.seg_offsets[lo + 1] ? lo : -1;
 }
 
 __device__ __forceinline__ void check_segment(const Params& p, int s) {
@@ -128,9 +145,8 @@ __global__ void __launch_bounds__(32 * COUNT_WARPS) balance_count_kernel(Params 
   const int warp = threadIdx.x / 32;
   const int32_t* ids = p.topk_idx + static_cast<long long>(t0) * p.k;
   const int n = (t1 - t0) * p.k;
-  // the entries in order, NTH apart, up to AHEAD of a thread's fetched before the
-  // first is used
-  constexpr int AHEAD = 8;
+  // the entries in order, NTH apart, all of a thread's fetched before the first is used
+  constexpr int AHEAD = 8 * COUNT_TOKENS / NTH;
   int id[AHEAD];
 #pragma unroll
   for (int u = 0; u < AHEAD; ++u) id[u] = threadIdx.x + u * NTH < n ? ids[threadIdx.x + u * NTH] : 0;
@@ -142,7 +158,10 @@ __global__ void __launch_bounds__(32 * COUNT_WARPS) balance_count_kernel(Params 
     on[u] = t < t1 && !(p.valid && !p.valid[t]);
   }
   for (int i = threadIdx.x; i < COUNT_WARPS * 129; i += NTH) (&hist[0][0])[i] = 0;
-  if (threadIdx.x >= NTH - 2) seg[threadIdx.x - (NTH - 2)] = segment_of(p, threadIdx.x == NTH - 1 ? t1 - 1 : t0);
+  if (warp < 2) {
+    const int s = segment_by_warp(p, warp ? t1 - 1 : t0, threadIdx.x & 31);
+    if ((threadIdx.x & 31) == 0) seg[warp] = s;
+  }
   __syncthreads();
   const int s0 = seg[0], s1 = seg[1];
   pdl_wait();  // the cleared counts
@@ -170,7 +189,6 @@ __global__ void __launch_bounds__(32 * COUNT_WARPS) balance_count_kernel(Params 
 #pragma unroll
   for (int u = 0; u < AHEAD; ++u)
     if (threadIdx.x + u * NTH < n) count(threadIdx.x + u * NTH, id[u]);
-  for (int i = threadIdx.x + AHEAD * NTH; i < n; i += NTH) count(i, ids[i]);
   __syncthreads();
   if (s0 >= 0)
     for (int i = threadIdx.x; i <= p.E; i += NTH) {
@@ -316,7 +334,8 @@ struct CountView {
 
 constexpr int LANE_WARPS = 8;   // of a CTA of the lane kernels
 constexpr int LANE_THREADS = 32 * LANE_WARPS;
-constexpr int LANE_STEPS = 8;   // steps of 32 / L tokens that a warp takes
+constexpr int LANE_CTAS = 4;    // per SM
+constexpr int MAX_STEPS = 32;   // of 32 / L tokens each that a warp takes
 
 // Tokens [first, end) in steps of 32 / L, a token on L = 2^lane_bits consecutive
 // lanes: lane l of them holds the C logits l C .. l C + C - 1, which lie in one
@@ -484,10 +503,10 @@ __device__ __forceinline__ void lane_totals(const Params& p, float* col, float g
 }
 
 template <int C, int ALIGN>
-__global__ void __launch_bounds__(LANE_THREADS, 4) balance_lanes_kernel(Params p) {
+__global__ void __launch_bounds__(LANE_THREADS, LANE_CTAS) balance_lanes_kernel(Params p) {
   __shared__ float sums[LANE_WARPS * 145];
   pdl_trigger();
-  const int per_warp = LANE_STEPS * (32 >> p.lane_bits);
+  const int per_warp = p.lane_steps * (32 >> p.lane_bits);
   const int first = (blockIdx.x * LANE_WARPS + (threadIdx.x >> 5)) * per_warp;
   float col[C], glob = 0.0f, loss = 0.0f;
 #pragma unroll
@@ -878,7 +897,14 @@ cudaError_t launch_lanes(Params p, cudaStream_t s) {
     KernelScope ks("balance", s);
     return launch_cluster(balance_small_lanes_kernel<C, ALIGN>, 1, CL, LANE_THREADS, (size_t)smem, s, p);
   }
-  const int per_cta = LANE_WARPS * LANE_STEPS * (32 >> p.lane_bits);
+  // One wave of CTAs where that leaves a warp at most MAX_STEPS steps, whose sums are
+  // fp32, and not fewer tokens than a tile.  64 experts, us, against 8 steps: 16384
+  // tokens 16.4 / 20.5, 262144 57 / 59, 10^6 133 / 141.
+  const int a_step = LANE_WARPS * (32 >> p.lane_bits);
+  const long long wave = static_cast<long long>(sm_count()) * LANE_CTAS * a_step;
+  p.lane_steps = static_cast<int>(std::min<long long>((p.T + wave - 1) / wave, MAX_STEPS));
+  p.lane_steps = std::max({p.lane_steps, TILE / a_step, 1});
+  const int per_cta = a_step * p.lane_steps;
   p.n_part = (p.T + per_cta - 1) / per_cta;
   e = launch_counts(p, s);
   if (e != cudaSuccess) return e;
