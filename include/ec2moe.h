@@ -408,8 +408,8 @@ size_t ec2moe_experts_fp8_workspace_size(const ec2moe_layer_desc* desc);
  *            (ec2moe_fp8_quantize with the inv_perm of ec2moe_route)
  *  slot_out  out [T * k, d] in desc->dtype: slot_out[t * k + s] =
  *            topk_w[t, s] * E_e(x_t) for e = topk_idx[t, s]
- * The hidden rows are the activation of the fp32 sums, quantised like
- * ec2moe_fp8_quantize's rows.  offsets, perm, topk_w and what happens to entries
+ * The hidden rows are the activation of the fp32 sums (GELU to within 1e-6 |u|),
+ * quantised like ec2moe_fp8_quantize's rows.  offsets, perm, topk_w and what happens to entries
  * out of range as for ec2moe_experts. */
 ec2moe_status ec2moe_experts_fp8(const ec2moe_layer_desc* desc, const void* Xq, const float* Xs,
                                  const int32_t* offsets, const ec2moe_fp8_weights* w, const float* topk_w,
@@ -481,9 +481,9 @@ int32_t ec2moe_last_launch_count(void);
  * "lr_encode", "lr_reduce", "lr_decode", "lr_codec", "expert_up", "expert_down", "shared_up",
  * "shared_down", "ffn_up", "ffn_down" (routed and shared experts in one launch),
  * "combine", "sum_counts", "quantize_rows", "quantize_blocks", "fp8_gemm", "fp8_up",
- * "fp8_down", "fp8_sum", "logits_prep", "logits_gemm", "logits_sum", "balance_clear",
- * "balance_count", "balance_main", "balance_final"); `ms` its device duration.  Profiling is off by default and
- * costs nothing when off. */
+ * "fp8_down", "fp8_sum", "logits_prep", "logits_gemm", "logits_sum", "balance",
+ * "balance_clear", "balance_count", "balance_main", "balance_final"); `ms` its device
+ * duration.  Profiling is off by default and costs nothing when off. */
 ec2moe_status ec2moe_profile_enable(int32_t enable);
 /* Restricts profiling to one launch per call: with launch_index >= 0 only the
  * kernel that is the launch_index-th launch (0-based) of each later call is

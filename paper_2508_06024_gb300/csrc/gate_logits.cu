@@ -5,17 +5,21 @@
 // bf16 activations: every fp32 gate row is split exactly into three bf16 terms
 // (w = w0 + w1 + w2, the rest below 2^-24 |w|) whose products with a bf16 value
 // are exact in fp32.  Up to 128 gate rows one kernel multiplies 128-token tiles by
-// all three, X w0 into a tensor-memory accumulator of its own.  The tensor core adds without rounding to nearest, so sums are kept
-// short: every 256 columns of d_model the accumulators are added to fp32 registers
-// while the next segment fills the other ones.  Few tokens: a cluster
-// of CTAs shares a tile's columns and adds its parts, in order, through
-// distributed shared memory.  What bounds long batches is the stream of X and, per
+// all three, X w0 into a tensor-memory accumulator of its own.  The tensor core adds
+// without rounding to nearest, so sums are kept short: every 256 columns of d_model
+// the accumulators are added to fp32 registers while the next segment fills the other
+// ones.  Few tokens: a cluster of CTAs shares a tile's columns and adds its parts, in
+// order, through distributed shared memory.  What bounds long batches is the stream of X and, per
 // tile, of the split rows (16 + 30 KB a 64-column block for 72 gate rows).
 //   warp 0 loads (TMA), warp 1 issues the MMAs, warps 2..5 drain; every wait is
 //   bounded.
 // More gate rows are a grouped-GEMM product of the terms in ranges of K, which a
 // last kernel adds in fp32 with the bias; fp32 activations take the fp32-accurate
 // GEMM.
+//
+// Measured: 16384 x 2048, 72 rows: 22.5 us for 72 MB (floor 10.7), of which the
+// split takes 3 before the product can start; 1024 x 768, 64 rows: 10 us, two
+// launches.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 

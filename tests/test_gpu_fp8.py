@@ -369,6 +369,42 @@ def test_experts(dtype, T, E, k, d, ff, act, allowed):
     assert err <= 3.6e-3 + (2.0 ** -9 if dtype == "bf16" else 0.0), err
 
 
+# Identity weights show the hidden rows: they are the exact activation's, rounded to
+# e4m3, except where that lies within GELU's and the scale's error of a tie.
+@pytest.mark.parametrize("T", [8, 200, 1000])
+def test_hidden_rows_are_the_exact_gelu_rounded(T):
+    rng = np.random.default_rng(T)
+    n = 128
+    q = rng.integers(0, 255, size=(T, n), dtype=np.uint8)
+    q[(q & 0x7F) == 0x7F] = 0
+    s = np.exp(rng.uniform(-9, -4, size=(T, 1))).astype(np.float32)
+    one, scale = cuda(np.where(np.eye(n), 0x38, 0).astype(np.uint8)), torch.ones(1, device="cuda")
+    w = C.make_fp8_weights(W1=one, S1=scale, W2=one, S2=scale)
+    desc = C.make_desc(T=T, d=n, E=1, d_ff=n, k=1, act=C.GELU, dtype=C.F32)
+    wsb = C.ec2moe_experts_fp8_workspace_size(desc)
+    out = torch.empty(T, n, device="cuda")
+    off = cuda(np.array([0, T], np.int32))
+    C.ec2moe_experts_fp8(desc, cuda(q), cuda(s), off, w, torch.ones(T, 1, device="cuda"),
+                         torch.arange(T, dtype=torch.int32, device="cuda"), out,
+                         torch.empty(wsb, dtype=torch.uint8, device="cuda"), wsb)
+    assert C.ec2moe_last_device_error() == C.OK
+    u = orc.e4m3_decode(q) * s.astype(np.float64)
+    g = orc.gelu(u)
+    to_grid = 448.0 / np.abs(g).max(axis=1, keepdims=True)
+    r = g * to_grid
+    codes = np.arange(256, dtype=np.uint8)
+    grid = np.unique(orc.e4m3_decode(codes[(codes & 0x7F) != 0x7F]))
+    at = np.clip(np.searchsorted(grid, r), 1, len(grid) - 1)
+    lo, hi = grid[at - 1], grid[at]
+    tie = (lo + hi) / 2
+    # GELU within 1e-6 |u|, the largest value (the scale) within 1e-6 of itself
+    sure = np.abs(r - tie) > 2e-6 * np.abs(u) * to_grid + 2e-6 * np.abs(r)
+    want = np.where(r < tie, lo, hi)
+    got = out.double().cpu().numpy() * to_grid
+    assert sure.mean() > 0.99
+    assert (np.abs(got - want)[sure] <= 1e-5 * np.abs(want)[sure] + 1e-12).all()
+
+
 # The products back from the hidden width by clusters that share it, scattered and
 # scaled by row.
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
