@@ -30,7 +30,7 @@
 // gradients; balance_final, the CTAs' partial sums in order.  Bounded by HBM for
 // long batches (the logits are read once, their gradients written once), by the
 // launches for short ones.  Measured: 1021 tokens of 16 experts 8.2 us; 262144 of 64
-// in 64 segments, 158 MB, 57 us, of which main 32 (floor 23) and the count 15.
+// in 64 segments, 158 MB, 46 us, of which main 32 (floor 23).
 #include <algorithm>
 
 #include <cuda_runtime.h>
@@ -47,7 +47,7 @@ namespace {
 
 constexpr int TILE = 128;       // tokens per tile
 constexpr int NT = 160;         // threads: a token each for TILE of them, 144 columns of logits for the moves
-constexpr int COUNT_TOKENS = 512;   // tokens per CTA of balance_count
+constexpr int COUNT_TOKENS = 256;   // tokens per CTA of balance_count
 constexpr int COUNT_WARPS = 8;
 constexpr int CL = 8;           // CTAs of the one-launch cluster
 constexpr long long SMALL_ENTRIES = 16384;
@@ -135,7 +135,10 @@ __device__ __forceinline__ void add_tokens(const Params& p, int s, int n) {
 }
 
 __global__ void __launch_bounds__(32 * COUNT_WARPS) balance_count_kernel(Params p) {
-  __shared__ int hist[COUNT_WARPS][128 + 1];  // of the CTA's first segment; [E]: its tokens
+  // of the CTA's first and last segment; [E]: its tokens.  Others' entries, of segments
+  // that lie inside the CTA's tokens, go to memory one by one (with the last one's
+  // too, 262144 tokens of 64 segments took 57 us, now 46).
+  __shared__ int hist[COUNT_WARPS][2][128 + 1];
   __shared__ int token_seg[COUNT_TOKENS];  // -1: does not count
   __shared__ int seg[2];
   pdl_trigger();
@@ -157,7 +160,7 @@ __global__ void __launch_bounds__(32 * COUNT_WARPS) balance_count_kernel(Params 
     const int t = t0 + threadIdx.x + u * NTH;
     on[u] = t < t1 && !(p.valid && !p.valid[t]);
   }
-  for (int i = threadIdx.x; i < COUNT_WARPS * 129; i += NTH) (&hist[0][0])[i] = 0;
+  for (int i = threadIdx.x; i < COUNT_WARPS * 2 * 129; i += NTH) (&hist[0][0][0])[i] = 0;
   if (warp < 2) {
     const int s = segment_by_warp(p, warp ? t1 - 1 : t0, threadIdx.x & 31);
     if ((threadIdx.x & 31) == 0) seg[warp] = s;
@@ -171,7 +174,7 @@ __global__ void __launch_bounds__(32 * COUNT_WARPS) balance_count_kernel(Params 
     const int s = on[u] ? segment_between(p, t0 + i, s0, s1) : -1;
     token_seg[i] = s;
     if (s < 0) continue;
-    if (s == s0) atomicAdd(&hist[warp][p.E], 1);
+    if (s == s0 || s == s1) atomicAdd(&hist[warp][s != s0][p.E], 1);
     else add_tokens(p, s, 1);
   }
   __syncthreads();
@@ -183,23 +186,25 @@ __global__ void __launch_bounds__(32 * COUNT_WARPS) balance_count_kernel(Params 
     const int s = token_seg[(i * per_k) >> 16];
     if (s < 0) return;
     if (e < 0 || e >= p.E) atomicOr(&g_balance_error, 1u);
-    else if (s == s0) atomicAdd(&hist[warp][e], 1);
+    else if (s == s0 || s == s1) atomicAdd(&hist[warp][s != s0][e], 1);
     else atomicAdd(&p.counts[static_cast<long long>(s) * p.E + e], 1);
   };
 #pragma unroll
   for (int u = 0; u < AHEAD; ++u)
     if (threadIdx.x + u * NTH < n) count(threadIdx.x + u * NTH, id[u]);
   __syncthreads();
-  if (s0 >= 0)
-    for (int i = threadIdx.x; i <= p.E; i += NTH) {
+  // a segment that is none (-1) has no entries here
+  const int half = threadIdx.x / (NTH / 2), s = half ? s1 : s0;
+  if (half == 0 || s1 != s0)
+    for (int i = threadIdx.x % (NTH / 2); i <= p.E; i += NTH / 2) {
       int v = 0;
 #pragma unroll
-      for (int w = 0; w < COUNT_WARPS; ++w) v += hist[w][i];
+      for (int w = 0; w < COUNT_WARPS; ++w) v += hist[w][half][i];
       if (v == 0) continue;
-      if (i < p.E) atomicAdd(&p.counts[static_cast<long long>(s0) * p.E + i], v);
-      else add_tokens(p, s0, v);
+      if (i < p.E) atomicAdd(&p.counts[static_cast<long long>(s) * p.E + i], v);
+      else add_tokens(p, s, v);
     }
-  for (int s = blockIdx.x * NTH + threadIdx.x; s < p.n_seg; s += gridDim.x * NTH) check_segment(p, s);
+  for (int i = blockIdx.x * NTH + threadIdx.x; i < p.n_seg; i += gridDim.x * NTH) check_segment(p, i);
 }
 
 // e^x for x <= 0 (or NaN), within 2^-22 + |x| 2^-24: a term of a softmax that
@@ -899,7 +904,7 @@ cudaError_t launch_lanes(Params p, cudaStream_t s) {
   }
   // One wave of CTAs where that leaves a warp at most MAX_STEPS steps, whose sums are
   // fp32, and not fewer tokens than a tile.  64 experts, us, against 8 steps: 16384
-  // tokens 16.4 / 20.5, 262144 57 / 59, 10^6 133 / 141.
+  // tokens 16.4 / 20.5, 10^6 in 100 segments 133 / 141.
   const int a_step = LANE_WARPS * (32 >> p.lane_bits);
   const long long wave = static_cast<long long>(sm_count()) * LANE_CTAS * a_step;
   p.lane_steps = static_cast<int>(std::min<long long>((p.T + wave - 1) / wave, MAX_STEPS));
