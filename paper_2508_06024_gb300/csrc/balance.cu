@@ -30,7 +30,7 @@
 // gradients; balance_final, the CTAs' partial sums in order.  Bounded by HBM for
 // long batches (the logits are read once, their gradients written once), by the
 // launches for short ones.  Measured: 1021 tokens of 16 experts 8.2 us; 262144 of 64
-// in 64 segments, 158 MB, 46 us, of which main 32 (floor 23).
+// in 64 segments, 158 MB, 45 us, of which main 31 (floor 23).
 #include <algorithm>
 
 #include <cuda_runtime.h>
@@ -137,7 +137,7 @@ __device__ __forceinline__ void add_tokens(const Params& p, int s, int n) {
 __global__ void __launch_bounds__(32 * COUNT_WARPS) balance_count_kernel(Params p) {
   // of the CTA's first and last segment; [E]: its tokens.  Others' entries, of segments
   // that lie inside the CTA's tokens, go to memory one by one (with the last one's
-  // too, 262144 tokens of 64 segments took 57 us, now 46).
+  // too, 262144 tokens of 64 segments took 57 us, without 46).
   __shared__ int hist[COUNT_WARPS][2][128 + 1];
   __shared__ int token_seg[COUNT_TOKENS];  // -1: does not count
   __shared__ int seg[2];
@@ -339,8 +339,10 @@ struct CountView {
 
 constexpr int LANE_WARPS = 8;   // of a CTA of the lane kernels
 constexpr int LANE_THREADS = 32 * LANE_WARPS;
-constexpr int LANE_CTAS = 4;    // per SM
-constexpr int MAX_STEPS = 32;   // of 32 / L tokens each that a warp takes
+// per SM: with 4 the eight-logit form's 78 registers are held to 64 (262144 tokens of
+// 16 experts 22.6 us, with 3 20.8; of 64 experts 46 and 45)
+constexpr int LANE_CTAS = 3;
+constexpr int MAX_STEPS = 24;   // of 32 / L tokens each that a warp takes
 
 // Tokens [first, end) in steps of 32 / L, a token on L = 2^lane_bits consecutive
 // lanes: lane l of them holds the C logits l C .. l C + C - 1, which lie in one
@@ -904,7 +906,7 @@ cudaError_t launch_lanes(Params p, cudaStream_t s) {
   }
   // One wave of CTAs where that leaves a warp at most MAX_STEPS steps, whose sums are
   // fp32, and not fewer tokens than a tile.  64 experts, us, against 8 steps: 16384
-  // tokens 16.4 / 20.5, 10^6 in 100 segments 133 / 141.
+  // tokens 16.4 / 20.5, 10^6 in 100 segments 131 / 141.
   const int a_step = LANE_WARPS * (32 >> p.lane_bits);
   const long long wave = static_cast<long long>(sm_count()) * LANE_CTAS * a_step;
   p.lane_steps = static_cast<int>(std::min<long long>((p.T + wave - 1) / wave, MAX_STEPS));
