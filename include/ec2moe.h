@@ -378,9 +378,9 @@ size_t ec2moe_fp8_gemm_workspace_size(int32_t n_groups, int32_t rows, int32_t N,
  *            elements (a multiple of 16 bytes)
  * Every block's products are summed in fp32 and the scaled sums of the blocks
  * added in fp32, rounded once to the output.  Rows of no group are not written; a
- * group whose range is not inside [0, rows] is skipped and
- * ec2moe_last_device_error then reports EC2MOE_ERR_INVALID_ARG.  No rows is a
- * no-op. */
+ * group whose range is not inside [0, rows], or which starts before the end of a group
+ * before it, is skipped and ec2moe_last_device_error then reports
+ * EC2MOE_ERR_INVALID_ARG.  No rows is a no-op. */
 ec2moe_status ec2moe_fp8_gemm(int32_t n_groups, int32_t rows, int32_t N, int32_t K, const void* A,
                               const float* A_scale, const int32_t* offsets, const void* B, const float* B_scale,
                               int32_t out_dtype, void* C, int64_t ldc, void* workspace, size_t ws_bytes,
@@ -410,7 +410,8 @@ size_t ec2moe_experts_fp8_workspace_size(const ec2moe_layer_desc* desc);
  *            topk_w[t, s] * E_e(x_t) for e = topk_idx[t, s]
  * The hidden rows are the activation of the fp32 sums (GELU to within 1e-6 |u|),
  * quantised like ec2moe_fp8_quantize's rows.  offsets, perm, topk_w and what happens to entries
- * out of range as for ec2moe_experts. */
+ * out of range as for ec2moe_experts; an expert whose rows start before the end of an
+ * earlier one's is skipped and reported too. */
 ec2moe_status ec2moe_experts_fp8(const ec2moe_layer_desc* desc, const void* Xq, const float* Xs,
                                  const int32_t* offsets, const ec2moe_fp8_weights* w, const float* topk_w,
                                  const int32_t* perm, void* slot_out, void* workspace, size_t ws_bytes,

@@ -24,6 +24,57 @@ __device__ __forceinline__ Fp8Scale fp8_scale(float m) {
   return Fp8Scale{__fdiv_rn(a, 448.0f), __fdiv_rn(448.0f, a)};
 }
 
+// First rows, row counts and the prefix of token tiles of TILE rows of G <= 32 CHUNKS
+// groups, from `offsets` (nullptr: one group of all rows).  One warp.  A range that is
+// not inside [0, rows] owns no rows; where there is one, ranges behind it may go over
+// the same rows again, so a group that starts before the end of one before it owns none
+// either: groups never own more than `rows` rows together, which grids and workspaces
+// are sized by.  err (nullptr: not reported): bit 1 is set when a range is skipped.
+template <int CHUNKS, int TILE>
+__device__ __forceinline__ void scan_group_rows(const int32_t* offsets, int G, int rows, int lane, int* row0, int* cnt,
+                                                int* prefix, unsigned int* err) {
+  int first[CHUNKS], n[CHUNKS];
+  bool bad = false;
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c) {
+    const int g = c * 32 + lane;
+    first[c] = 0;
+    n[c] = g < G ? rows : 0;
+    if (offsets && g < G) {
+      const int a = offsets[g], b = offsets[g + 1];
+      const bool in = a >= 0 && a <= b && b <= rows;
+      first[c] = in ? a : 0;
+      n[c] = in ? b - a : 0;
+      bad |= !in;
+    }
+  }
+  // ranges that are all in place do not decrease, so they cannot overlap
+  if (__any_sync(0xffffffffu, bad)) {
+    if (err && lane == 0) atomicOr(err, 2u);
+    int reach = 0;  // where the groups of the chunks before end
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+      int end = n[c] > 0 ? first[c] + n[c] : 0;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, end, o);
+        if (lane >= o) end = max(end, y);
+      }
+      int before = __shfl_up_sync(0xffffffffu, end, 1);
+      before = lane == 0 ? reach : max(before, reach);
+      if (first[c] < before) n[c] = 0;
+      reach = max(reach, __shfl_sync(0xffffffffu, end, 31));
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c)
+    if (c * 32 + lane < G) {
+      row0[c * 32 + lane] = first[c];
+      cnt[c * 32 + lane] = n[c];
+    }
+  warp_exclusive_scan<CHUNKS>(G, lane, [&](int g) { return (cnt[g] + TILE - 1) / TILE; }, prefix);
+}
+
 // Two values, scaled, as e4m3 (lo in the low byte).
 __device__ __forceinline__ uint32_t fp8_pack2(float lo, float hi, float inv) {
   return __nv_cvt_float2_to_fp8x2(make_float2(lo * inv, hi * inv), __NV_SATFINITE, __NV_E4M3);

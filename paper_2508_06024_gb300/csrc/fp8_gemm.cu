@@ -211,25 +211,8 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
   if (warp == 0) {
     pdl_wait();
     // Per-group first rows and tile prefix (m tiles), one warp-wide scan.
-    warp_exclusive_scan<(MAX_GROUPS + 31) / 32>(
-        p.G, lane,
-        [&](int g) {
-          int r0 = 0, mg = p.rows;
-          if (p.offsets) {
-            r0 = p.offsets[g];
-            mg = p.offsets[g + 1] - r0;
-            if (r0 < 0 || mg < 0 || static_cast<long long>(r0) + mg > p.rows) {
-              // not a range of this call's rows: the group is skipped
-              atomicOr(&g_fp8_error, 2u);
-              r0 = 0;
-              mg = 0;
-            }
-          }
-          row0[g] = r0;
-          row_cnt[g] = mg;
-          return (mg + C::TILE_M - 1) / C::TILE_M;
-        },
-        tile_prefix);
+    scan_group_rows<(MAX_GROUPS + 31) / 32, C::TILE_M>(p.offsets, p.G, p.rows, lane, row0, row_cnt, tile_prefix,
+                                                       &g_fp8_error);
   }
   if (warp == 0 && lane == 0) {
     tma_prefetch_desc(&tmA);

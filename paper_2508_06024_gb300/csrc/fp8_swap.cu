@@ -66,25 +66,8 @@ struct Params {
 
 // First rows, row counts and token-tile prefix of the groups (one warp).
 __device__ __forceinline__ void scan_groups(const Shape& s, int lane, int* row0, int* cnt, int* prefix, bool report) {
-  warp_exclusive_scan<(MAX_GROUPS + 31) / 32>(
-      s.G, lane,
-      [&](int g) {
-        int r0 = 0, mg = s.rows;
-        if (s.offsets) {
-          r0 = s.offsets[g];
-          mg = s.offsets[g + 1] - r0;
-          if (r0 < 0 || mg < 0 || static_cast<long long>(r0) + mg > s.rows) {
-            // not a range of this call's rows: the group is skipped
-            if (report) atomicOr(&g_fp8_swap_error, 2u);
-            r0 = 0;
-            mg = 0;
-          }
-        }
-        row0[g] = r0;
-        cnt[g] = mg;
-        return (mg + ROWS - 1) / ROWS;
-      },
-      prefix);
+  scan_group_rows<(MAX_GROUPS + 31) / 32, ROWS>(s.offsets, s.G, s.rows, lane, row0, cnt, prefix,
+                                                report ? &g_fp8_swap_error : nullptr);
 }
 
 struct Tile {
@@ -510,7 +493,9 @@ __global__ void __launch_bounds__(256) fp8_swap_sum_kernel(const SumParams p) {
 }
 
 // ------------------------------------------------------------------ host side
-// Token tiles that the groups can hold at most.
+// Token tiles that the groups can hold at most: they own `rows` rows together at
+// most, whatever `offsets` says (scan_group_rows), and the partial sums' space is
+// sized by this.
 long long token_tiles(int G, int rows) { return (rows < G ? rows : G) + rows / ROWS; }
 
 }  // namespace
