@@ -86,11 +86,10 @@ __device__ __forceinline__ float silu_bf16out(float u) { return __fdividef(u, 1.
 // the total, which every lane returns.  All values are fetched before the
 // scan, so reading them from global memory costs about one memory latency
 // instead of n dependent ones.  copy (optional, global) receives out[0..n].
-template <int CHUNKS, typename F>
-__device__ __forceinline__ int warp_exclusive_scan(int n, int lane, F value, int* out, int* copy = nullptr) {
-  int v[CHUNKS];
-#pragma unroll
-  for (int c = 0; c < CHUNKS; ++c) v[c] = c * 32 + lane < n ? value(c * 32 + lane) : 0;
+// First the form with the values at hand: lane l holds values l, 32 + l, ...
+template <int CHUNKS>
+__device__ __forceinline__ int warp_exclusive_scan(int n, int lane, const int (&v)[CHUNKS], int* out,
+                                                   int* copy = nullptr) {
   int carry = 0;
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c) {
@@ -113,6 +112,13 @@ __device__ __forceinline__ int warp_exclusive_scan(int n, int lane, F value, int
     if (copy) copy[n] = carry;
   }
   return carry;
+}
+template <int CHUNKS, typename F>
+__device__ __forceinline__ int warp_exclusive_scan(int n, int lane, F value, int* out, int* copy = nullptr) {
+  int v[CHUNKS];
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c) v[c] = c * 32 + lane < n ? value(c * 32 + lane) : 0;
+  return warp_exclusive_scan(n, lane, v, out, copy);
 }
 
 }  // namespace ec2moe

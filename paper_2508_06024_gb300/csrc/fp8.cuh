@@ -67,12 +67,14 @@ __device__ __forceinline__ void scan_group_rows(const int32_t* offsets, int G, i
     }
   }
 #pragma unroll
-  for (int c = 0; c < CHUNKS; ++c)
+  for (int c = 0; c < CHUNKS; ++c) {
     if (c * 32 + lane < G) {
       row0[c * 32 + lane] = first[c];
       cnt[c * 32 + lane] = n[c];
     }
-  warp_exclusive_scan<CHUNKS>(G, lane, [&](int g) { return (cnt[g] + TILE - 1) / TILE; }, prefix);
+    n[c] = (n[c] + TILE - 1) / TILE;
+  }
+  warp_exclusive_scan(G, lane, n, prefix);
 }
 
 // Two values, scaled, as e4m3 (lo in the low byte).
