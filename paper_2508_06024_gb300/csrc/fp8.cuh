@@ -48,32 +48,35 @@ __device__ __forceinline__ void scan_group_rows(const int32_t* offsets, int G, i
       bad |= !in;
     }
   }
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c)
+    if (c * 32 + lane < G) {
+      row0[c * 32 + lane] = first[c];
+      cnt[c * 32 + lane] = n[c];
+    }
   // ranges that are all in place do not decrease, so they cannot overlap
   if (__any_sync(0xffffffffu, bad)) {
     if (err && lane == 0) atomicOr(err, 2u);
-    int reach = 0;  // where the groups of the chunks before end
-#pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) {
-      int end = n[c] > 0 ? first[c] + n[c] : 0;
-#pragma unroll
+    int reach = 0;  // where the groups before end
+#pragma unroll 1
+    for (int g = lane; g - lane < G; g += 32) {
+      const int from = g < G ? row0[g] : 0, rows_of = g < G ? cnt[g] : 0;
+      int end = rows_of > 0 ? from + rows_of : 0;
+#pragma unroll 1
       for (int o = 1; o < 32; o <<= 1) {
         const int y = __shfl_up_sync(0xffffffffu, end, o);
         if (lane >= o) end = max(end, y);
       }
       int before = __shfl_up_sync(0xffffffffu, end, 1);
       before = lane == 0 ? reach : max(before, reach);
-      if (first[c] < before) n[c] = 0;
+      if (g < G && from < before) cnt[g] = 0;
       reach = max(reach, __shfl_sync(0xffffffffu, end, 31));
     }
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) n[c] = c * 32 + lane < G ? cnt[c * 32 + lane] : 0;
   }
 #pragma unroll
-  for (int c = 0; c < CHUNKS; ++c) {
-    if (c * 32 + lane < G) {
-      row0[c * 32 + lane] = first[c];
-      cnt[c * 32 + lane] = n[c];
-    }
-    n[c] = (n[c] + TILE - 1) / TILE;
-  }
+  for (int c = 0; c < CHUNKS; ++c) n[c] = (n[c] + TILE - 1) / TILE;
   warp_exclusive_scan(G, lane, n, prefix);
 }
 
