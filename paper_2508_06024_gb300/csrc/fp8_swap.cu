@@ -134,6 +134,9 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
   uint64_t* drain = sempty + RING;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::OFF_SLOT);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  // what the roles leave in flight when they end: the producer's stages (low half) and the
+  // phases that they complete, the lane + 1 of the MMA warp that issued MMAs
+  volatile uint32_t* in_flight = tmem_slot + 2;
   int* prefix = reinterpret_cast<int*>(smem + C::OFF_PREFIX);
   int* row0 = reinterpret_cast<int*>(smem + C::OFF_ROW0);
   int* cnt = reinterpret_cast<int*>(smem + C::OFF_CNT);
@@ -156,6 +159,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
     }
     mbar_init(smem_u32(drain), 1);
     *abort_flag = 0;
+    in_flight[0] = in_flight[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -195,8 +199,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
     const bool issue = elect_one();
     int stage = 0;
     uint32_t phase = 0;
-    uint32_t issued = 0;  // bit s: stage s holds a copy the consumer has not released
-    uint32_t issued_phase = 0;
+    uint32_t issued = 0, issued_phase = 0;  // bit s: stage s holds a copy, the phase that it completes
     int cursor = 0, tile = tile0, kb = kb_first;
     bool ok = true;
     Tile t{};
@@ -252,11 +255,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
         phase ^= 1u;
       }
     }
-    if (!ok || *abort_flag) {
-      // Let every copy this CTA started land before shared memory is released.
-      for (int s = 0; s < STAGES; ++s)
-        if (issued & (1u << s)) mbar_drain(smem_u32(&full[s]), (issued_phase >> s) & 1u, DRAIN_CYCLES);
-    }
+    if (lane == 0) in_flight[0] = issued | (issued_phase << 16);
   } else if (warp == 1) {
     // ---------------------------------------------------------------- MMA issuer
     const bool issue = elect_one();
@@ -292,11 +291,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
         bph ^= 1u;
       }
     }
-    if ((!ok || *abort_flag) && any && issue) {
-      // All MMAs issued so far must finish before TMEM is freed.
-      umma_commit(smem_u32(drain));
-      mbar_drain(smem_u32(drain), 0, DRAIN_CYCLES);
-    }
+    if (any && issue) in_flight[1] = lane + 1;
   } else if (warp == 2) {
     // ------------------------------------------------------------------ scales
     pdl_wait();  // the rows' scales
@@ -391,6 +386,16 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
 
   tc_fence_before();
   __syncthreads();
+  if (*abort_flag) {  // no warp waits any more: the same in all of them
+    if (warp == 0) {
+      drain_copies(smem_u32(full), in_flight[0] & 0xffffu, in_flight[0] >> 16);
+    } else if (warp == 1 && in_flight[1] == lane + 1u) {
+      // the thread that issued the MMAs: a commit covers its own
+      umma_commit(smem_u32(drain));
+      mbar_drain(smem_u32(drain), 0, DRAIN_CYCLES);
+    }
+    __syncthreads();
+  }
   if (warp == 1) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(C::TMEM_COLS) : "memory");

@@ -136,6 +136,9 @@ __global__ void __launch_bounds__(LG_THREADS, 1)
   uint64_t* drain = tempty + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  // what the roles leave in flight when they end: the producer's stages (low half) and the
+  // phases that they complete, the lane + 1 of the MMA warp that issued MMAs
+  volatile uint32_t* in_flight = tmem_slot + 2;
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
   const int cs = p.cs;
@@ -158,6 +161,7 @@ __global__ void __launch_bounds__(LG_THREADS, 1)
     }
     mbar_init(smem_u32(drain), 1);
     *abort_flag = 0;
+    in_flight[0] = in_flight[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -202,6 +206,7 @@ __global__ void __launch_bounds__(LG_THREADS, 1)
     pdl_wait();
     if (issue)
       for (int c = 0; c < pre; ++c) load_w(c, c);
+    // bit s: stage s holds a copy, the phase that it completes
     uint32_t issued = pre ? (1u << pre) - 1u : 0u, issued_phase = 0;
     int stage = pre == S ? 0 : pre;
     uint32_t phase = pre == S ? 1u : 0u;
@@ -219,11 +224,7 @@ __global__ void __launch_bounds__(LG_THREADS, 1)
         phase ^= 1u;
       }
     }
-    if (!ok || *abort_flag) {
-      // Let every copy this CTA started land before shared memory is released.
-      for (int s = 0; s < S; ++s)
-        if (issued & (1u << s)) mbar_drain(smem_u32(&full[s]), (issued_phase >> s) & 1u, DRAIN_CYCLES);
-    }
+    if (lane == 0) in_flight[0] = issued | (issued_phase << 16);
   } else if (warp == 1) {
     // ---------------------------------------------------------------- MMA issuer
     const bool issue = elect_one();
@@ -267,11 +268,7 @@ __global__ void __launch_bounds__(LG_THREADS, 1)
         if (ok && issue) umma_commit(smem_u32(&tfull[buf]));
       }
     }
-    if ((!ok || *abort_flag) && any && issue) {
-      // All MMAs issued so far must finish before TMEM is freed.
-      umma_commit(smem_u32(drain));
-      mbar_drain(smem_u32(drain), 0, DRAIN_CYCLES);
-    }
+    if (any && issue) in_flight[1] = lane + 1;
   } else {
     // -------------------------------------------------------------------- drain
     const int q = warp & 3;
@@ -339,6 +336,16 @@ __global__ void __launch_bounds__(LG_THREADS, 1)
 
   tc_fence_before();
   __syncthreads();
+  if (*abort_flag) {  // no warp waits any more: the same in all of them
+    if (warp == 0) {
+      drain_copies(smem_u32(full), in_flight[0] & 0xffffu, in_flight[0] >> 16);
+    } else if (warp == 1 && in_flight[1] == lane + 1u) {
+      // the thread that issued the MMAs: a commit covers its own
+      umma_commit(smem_u32(drain));
+      mbar_drain(smem_u32(drain), 0, DRAIN_CYCLES);
+    }
+    __syncthreads();
+  }
   if (warp == 1) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");

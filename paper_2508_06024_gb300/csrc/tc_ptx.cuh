@@ -92,6 +92,19 @@ __device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity, long l
   }
 }
 
+// What a CTA has in flight when one of its waits gave up.  Any of its warps can be the
+// one that gives up, after the producer and the MMA issuer have issued their last, so
+// this is asked once all warps have ended their roles (a __syncthreads after them) and
+// before shared memory and TMEM are released.
+//
+// The copies of a pipeline: stages of `issued`, the parity that each one's barrier
+// (full0 + 8 stage) completes with them in issued_phase.
+__device__ __forceinline__ void drain_copies(uint32_t full0, uint32_t issued, uint32_t issued_phase) {
+  const long long t0 = clock64();
+  for (int s = 0; issued >> s; ++s)
+    if ((issued >> s) & 1u) mbar_drain(full0 + 8u * s, (issued_phase >> s) & 1u, DRAIN_CYCLES - (clock64() - t0));
+}
+
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* tm, int x, int y, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
@@ -291,6 +304,13 @@ __device__ __forceinline__ void st_async_v4(uint32_t cluster_addr, float a, floa
 __device__ __forceinline__ void st_cluster_v4(uint32_t cluster_addr, float a, float b, float c, float d) {
   asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(cluster_addr), "f"(a), "f"(b), "f"(c), "f"(d)
                : "memory");
+}
+// Raises the abort flag of the pair's other CTA where this one's is up; a cluster
+// barrier behind it makes the pair agree.
+__device__ __forceinline__ void abort_pair(volatile int* abort_flag, uint32_t rank) {
+  if (*abort_flag)
+    asm volatile("st.shared::cluster.s32 [%0], 1;" ::"r"(map_to_rank(smem_u32(const_cast<int*>(abort_flag)), rank ^ 1u))
+                 : "memory");
 }
 // Four fp32 words from the shared memory of a CTA of the cluster (shared::cluster
 // address, 16-byte aligned), written before a cluster barrier.
