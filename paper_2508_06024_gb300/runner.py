@@ -98,6 +98,8 @@ class Fp8LayerRun:
             C.ec2moe_fp8_quantize(cfg.dtype, E, rows, cols, cols, w, C.FP8_BLOCK, None, 0, q, s)
             self.quantised["W" + i], self.quantised["S" + i] = q, s
         self.weights = C.make_fp8_weights(**self.quantised)
+        # calls may run on any stream, and nothing orders those behind this one
+        torch.cuda.current_stream().synchronize()
 
         self.Y, self.slot = empty(T, d, dtype=dt), empty(n, d, dtype=dt)
         self.topk_idx, self.topk_w = empty(T, k, dtype=torch.int32), empty(T, k)
