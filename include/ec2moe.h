@@ -380,7 +380,8 @@ size_t ec2moe_fp8_gemm_workspace_size(int32_t n_groups, int32_t rows, int32_t N,
  * added in fp32, rounded once to the output.  Rows of no group are not written; a
  * group whose range is not inside [0, rows], or which starts before the end of a group
  * before it, is skipped and ec2moe_last_device_error then reports
- * EC2MOE_ERR_INVALID_ARG.  No rows is a no-op. */
+ * EC2MOE_ERR_INVALID_ARG.  No rows is a no-op; more than 2^31 - 256 of them
+ * return EC2MOE_ERR_UNSUPPORTED. */
 ec2moe_status ec2moe_fp8_gemm(int32_t n_groups, int32_t rows, int32_t N, int32_t K, const void* A,
                               const float* A_scale, const int32_t* offsets, const void* B, const float* B_scale,
                               int32_t out_dtype, void* C, int64_t ldc, void* workspace, size_t ws_bytes,

@@ -572,6 +572,8 @@ ec2moe_status check_fp8_shape(int n_groups, int rows, int N, int K) {
   if (n_groups <= 0 || rows < 0 || N <= 0 || K <= 0) return EC2MOE_ERR_INVALID_ARG;
   if (n_groups > EC2MOE_MAX_EXPERTS) return EC2MOE_ERR_UNSUPPORTED;
   if (N % 16 != 0 || K % 16 != 0) return EC2MOE_ERR_MISALIGNED;
+  // row indexes are 32-bit up to the end of the last tile, of 256 rows
+  if (rows > 0x7fffffff - 255) return EC2MOE_ERR_UNSUPPORTED;
   // rows of B, and tiles of C (of 128 x 128 at least, a partial one per group)
   if ((long long)n_groups * N > 0x7fffffffLL) return EC2MOE_ERR_UNSUPPORTED;
   if (((long long)rows / 128 + n_groups) * ((N + 127) / 128) > 0x7fffffffLL) return EC2MOE_ERR_UNSUPPORTED;
