@@ -1133,6 +1133,8 @@ ec2moe_status ec2moe_fp8_quantize(int32_t dtype, int32_t n_mats, int32_t rows, i
   const long long n_kb = (cols + EC2MOE_FP8_BLOCK - 1) / EC2MOE_FP8_BLOCK;
   // rows and launch sizes are 32-bit
   if (n > 0x7fffffffLL || n * (k > 0 ? k : 1) > 0x7fffffffLL || n * n_kb > 0x7fffffffLL) return EC2MOE_ERR_UNSUPPORTED;
+  // so are a matrix's rows up to the end of its last block
+  if (block_rows == EC2MOE_FP8_BLOCK && rows > 0x7fffffff - (EC2MOE_FP8_BLOCK - 1)) return EC2MOE_ERR_UNSUPPORTED;
   if (n == 0) return EC2MOE_OK;
   EC2MOE_REQUIRE_PTR(X);
   EC2MOE_REQUIRE_PTR(Q);

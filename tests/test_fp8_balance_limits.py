@@ -26,3 +26,9 @@ def test_product_rows_whose_last_tile_passes_32_bits(rows):
     """A tile of 256 rows begins at most 255 before the end of the rows and ends behind it."""
     assert status(C.ec2moe_fp8_gemm, 1, rows, 16, 16, A, A, None, A, A, C.BF16, A, 16, A, 0, 0) == C.ERR_UNSUPPORTED
     assert C.ec2moe_fp8_gemm_workspace_size(1, rows, 16, 16) == 0
+
+
+@pytest.mark.parametrize("rows", [LAST, LAST - 1, LAST - 126])
+def test_weight_rows_whose_last_block_passes_32_bits(rows):
+    """A block of 128 weight rows begins at most 127 before the end of a matrix and ends behind it."""
+    assert status(C.ec2moe_fp8_quantize, C.BF16, 1, rows, 16, 16, A, 128, None, 0, A, A, 0) == C.ERR_UNSUPPORTED
