@@ -431,7 +431,8 @@ ec2moe_status ec2moe_gate_logits(const ec2moe_layer_desc* desc, const void* X, c
                                  const float* b_local, const float* W_global, const float* b_global, float* logits,
                                  void* workspace, size_t ws_bytes, ec2moe_stream_t stream);
 
-/* Bytes of device workspace ec2moe_balance_loss needs (0 on an invalid desc or n_seg < 1). */
+/* Bytes of device workspace ec2moe_balance_loss needs (0 on an invalid desc or n_seg).
+ * 1 <= n_seg <= 2^30, n_seg * E < 2^31. */
 size_t ec2moe_balance_loss_workspace_size(const ec2moe_layer_desc* desc, int32_t n_seg);
 
 /* Per-expert counts, the balance loss of the gate and its gradients.

@@ -1291,8 +1291,14 @@ ec2moe_status ec2moe_gate_logits(const ec2moe_layer_desc* desc, const void* X, c
   return EC2MOE_OK;
 }
 
+// The counts' index, and the sum of two segment numbers in the search for a token's,
+// are 32-bit.
+static bool balance_segments_fit(int32_t n_seg, int32_t E) {
+  return n_seg <= 1 << 30 && (long long)n_seg * E <= 0x7fffffffLL;
+}
+
 size_t ec2moe_balance_loss_workspace_size(const ec2moe_layer_desc* desc, int32_t n_seg) {
-  if (check_desc(desc) != EC2MOE_OK || n_seg < 1) return 0;
+  if (check_desc(desc) != EC2MOE_OK || n_seg < 1 || !balance_segments_fit(n_seg, desc->E)) return 0;
   return balance_bytes(desc->T, desc->E, desc->n_groups, n_seg);
 }
 
@@ -1309,7 +1315,7 @@ ec2moe_status ec2moe_balance_loss(const ec2moe_layer_desc* desc, const float* lo
   if (st != EC2MOE_OK) return st;
   const int O = desc->E + (desc->n_groups > 1 ? desc->n_groups : 0);
   if (n_seg < 1 || (!seg_offsets && n_seg != 1) || ld < O) return EC2MOE_ERR_INVALID_ARG;
-  if ((long long)n_seg * desc->E > 0x7fffffffLL) return EC2MOE_ERR_UNSUPPORTED;
+  if (!balance_segments_fit(n_seg, desc->E)) return EC2MOE_ERR_UNSUPPORTED;
   if (!loss || !counts) return EC2MOE_ERR_INVALID_ARG;
   if (desc->T > 0 && (!logits || !topk_idx)) return EC2MOE_ERR_INVALID_ARG;
   if (!workspace || ws_bytes < ec2moe_balance_loss_workspace_size(desc, n_seg)) return EC2MOE_ERR_WORKSPACE;

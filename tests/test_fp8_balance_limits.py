@@ -32,3 +32,12 @@ def test_product_rows_whose_last_tile_passes_32_bits(rows):
 def test_weight_rows_whose_last_block_passes_32_bits(rows):
     """A block of 128 weight rows begins at most 127 before the end of a matrix and ends behind it."""
     assert status(C.ec2moe_fp8_quantize, C.BF16, 1, rows, 16, 16, A, 128, None, 0, A, A, 0) == C.ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("n_seg", [LAST, (1 << 30) + 1])
+def test_segments_whose_search_passes_32_bits(n_seg):
+    """The search for a token's segment adds two segment numbers."""
+    desc = C.make_desc(T=64, d=256, E=1, d_ff=0, k=1, n_groups=1)
+    assert status(C.ec2moe_balance_loss, desc, A, 1, bytes([1]), A, None, A, n_seg, 0.01, None, A, A, None, None, A, 1 << 60,
+                  0) == C.ERR_UNSUPPORTED
+    assert C.ec2moe_balance_loss_workspace_size(desc, n_seg) == 0
