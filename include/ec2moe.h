@@ -426,7 +426,9 @@ size_t ec2moe_gate_logits_workspace_size(const ec2moe_layer_desc* desc);
 
 /* The gate's logits to fp32 accuracy: logits[t] = (W_local x_t + b_local,
  * W_global x_t + b_global), fp32 [T, E + K] (K = n_groups; [T, E] when it is 1).
- * Passage: Eq. 5 and Eq. 6 before their softmaxes. */
+ * Passage: Eq. 5 and Eq. 6 before their softmaxes.  Infinities and NaN in x_t, the gate
+ * rows and the biases give what the definition gives; they reach the logits of their own
+ * token or gate row alone. */
 ec2moe_status ec2moe_gate_logits(const ec2moe_layer_desc* desc, const void* X, const float* W_local,
                                  const float* b_local, const float* W_global, const float* b_global, float* logits,
                                  void* workspace, size_t ws_bytes, ec2moe_stream_t stream);

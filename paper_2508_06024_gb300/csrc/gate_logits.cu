@@ -13,6 +13,9 @@
 // tile, of the split rows (16 + 30 KB a 64-column block for 72 gate rows).
 //   warp 0 loads (TMA), warp 1 issues the MMAs, warps 2..5 drain; every wait is
 //   bounded.
+// A result that is not finite says nothing: with an infinity in X (or a weight beyond
+// bf16's range) terms of both signs, and terms of 0, give NaN where the definition has
+// an infinity.  Such results are computed again from X and the fp32 gate rows.
 // More gate rows are a grouped-GEMM product of the terms in ranges of K, which a
 // last kernel adds in fp32 with the bias; fp32 activations take the fp32-accurate
 // GEMM.
@@ -40,6 +43,47 @@ constexpr int RANGE = 512;  // columns of X that the grouped GEMM sums on the te
 // Gate row o (local rows, then global ones) of length d.
 __device__ __forceinline__ const float* gate_row(const float* W_local, const float* W_global, int E, int d, int o) {
   return o < E ? W_local + static_cast<size_t>(o) * d : W_global + static_cast<size_t>(o - E) * d;
+}
+
+__device__ __forceinline__ bool finite(float v) { return fabsf(v) < INFINITY; }
+
+// What the gate's logits are made of.
+struct Source {
+  const __nv_bfloat16* X;
+  const float* W_local;
+  const float* W_global;
+  const float* b_local;
+  const float* b_global;
+  int E, O, d;
+};
+// Computes again, in 64 bits, the results that are not finite of those that a warp
+// stored: out[i], the logit i % O of token t0 + i / O, for i = first + lane, first + lane +
+// step, ... below n.  Kept out of line: few calls come here, and short ones are mostly
+// fetching their code.
+__device__ __noinline__ void mend_not_finite(const Source& src, float* out, long long n, long long first, int step,
+                                             long long t0) {
+  const int lane = threadIdx.x & 31;
+  for (long long i0 = first; i0 < n; i0 += step) {
+    uint32_t m = __ballot_sync(0xffffffffu, i0 + lane < n && !finite(out[i0 + lane]));
+    for (; m; m &= m - 1) {
+      const long long i = i0 + __ffs(m) - 1, t = t0 + i / src.O;
+      const int o = static_cast<int>(i % src.O);
+      const __nv_bfloat16* x = src.X + t * src.d;
+      const float* w = gate_row(src.W_local, src.W_global, src.E, src.d, o);
+      double s = 0.0;
+      for (int c = 4 * lane; c < src.d; c += 128) {
+        const uint2 xv = *reinterpret_cast<const uint2*>(x + c);
+        const float4 wv = *reinterpret_cast<const float4*>(w + c);
+        s += static_cast<double>(bf16_lo(xv.x)) * wv.x;
+        s += static_cast<double>(bf16_hi(xv.x)) * wv.y;
+        s += static_cast<double>(bf16_lo(xv.y)) * wv.z;
+        s += static_cast<double>(bf16_hi(xv.y)) * wv.w;
+      }
+#pragma unroll
+      for (int j = 16; j > 0; j >>= 1) s += __shfl_xor_sync(0xffffffffu, s, j);
+      if (lane == 0) out[i] = static_cast<float>(s + (o < src.E ? src.b_local[o] : src.b_global[o - src.E]));
+    }
+  }
 }
 
 // terms[j * pad + o][c] = term j of gate row o, 0 for O <= o < pad; four columns per
@@ -80,19 +124,27 @@ __global__ void __launch_bounds__(256) logits_rows_kernel(const float* W_local, 
 }
 
 // logits[t][o] = bias + the sum over ranges and terms of part[range][t][term * O + o] (pitch N).
-__global__ void __launch_bounds__(256) logits_sum_kernel(const float* part, int ranges, int terms, int N, int T, int E,
-                                                         int O, const float* b_local, const float* b_global,
-                                                         float* logits) {
+// src.X: the activations where the sums are of terms (nullptr: they are the products' own).
+__global__ void __launch_bounds__(256) logits_sum_kernel(const float* part, int ranges, int terms, int N, int T,
+                                                         const __grid_constant__ Source src, float* logits) {
   pdl_trigger();
   pdl_wait();
-  const long long i = blockIdx.x * 256LL + threadIdx.x;
-  if (i >= static_cast<long long>(T) * O) return;
-  const long long t = i / O;
-  const int o = static_cast<int>(i - t * O);
-  float v = o < E ? b_local[o] : b_global[o - E];
-  for (int j = terms - 1; j >= 0; --j)
-    for (int r = 0; r < ranges; ++r) v += part[(static_cast<long long>(r) * T + t) * N + j * O + o];
-  logits[i] = v;
+  const int O = src.O;
+  const long long n = static_cast<long long>(T) * O, i = blockIdx.x * 256LL + threadIdx.x;
+  bool all = true;
+  if (i < n) {
+    const long long t = i / O;
+    const int o = static_cast<int>(i - t * O);
+    float v = o < src.E ? src.b_local[o] : src.b_global[o - src.E];
+    for (int j = terms - 1; j >= 0; --j)
+      for (int r = 0; r < ranges; ++r) v += part[(static_cast<long long>(r) * T + t) * N + j * O + o];
+    logits[i] = v;
+    all = finite(v);
+  }
+  if (__any_sync(0xffffffffu, !all) && src.X) {
+    const long long first = i - (threadIdx.x & 31);
+    mend_not_finite(src, logits, first + 32 < n ? first + 32 : n, first, 32, 0);
+  }
 }
 
 // ------------------------------------------------------------- the fused kernel
@@ -109,6 +161,7 @@ struct LgParams {
   const float* b_local;
   const float* b_global;
   float* logits;
+  Source src;
   int T, E, O, pad, nk, cs, stages, pitch;
   long long timeout;
 };
@@ -120,7 +173,8 @@ int lg_smem(int pad, int pitch, int stages) {
 
 template <int NB>  // blocks of 16 gate rows
 __global__ void __launch_bounds__(LG_THREADS, 1)
-    logits_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW, const LgParams p) {
+    logits_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW,
+                     const __grid_constant__ LgParams p) {
   // up to 80 gate rows the three terms are one MMA of 3 pad <= 240 columns, with an
   // accumulator each (16384 x 2048, 72 rows: 26.6 -> 20.5 us)
   constexpr bool WIDE = NB <= 5;
@@ -320,9 +374,12 @@ __global__ void __launch_bounds__(LG_THREADS, 1)
       float* out = p.logits + static_cast<long long>(tile) * BM * p.O;
       int r = (threadIdx.x - 64) / p.O, c = (threadIdx.x - 64) - r * p.O;
       const int dr = 128 / p.O, dc = 128 - dr * p.O;
+      bool all = true;  // results are finite
 #pragma unroll 4
       for (int i = threadIdx.x - 64; i < n; i += 128) {
-        out[i] = tile_out[r * p.pitch + c];
+        const float v = tile_out[r * p.pitch + c];
+        out[i] = v;
+        all &= finite(v);
         r += dr;
         c += dc;
         if (c >= p.O) {
@@ -330,6 +387,8 @@ __global__ void __launch_bounds__(LG_THREADS, 1)
           ++r;
         }
       }
+      if (__any_sync(0xffffffffu, !all))
+        mend_not_finite(p.src, out, n, threadIdx.x - 64 - lane, 128, static_cast<long long>(tile) * BM);
       asm volatile("bar.sync 1, 128;" ::: "memory");
     }
   }
@@ -358,6 +417,7 @@ __global__ void __launch_bounds__(LG_THREADS, 1)
     const int left = p.T - tile_first * BM - first;
     const int n = (left < rows ? left : rows) * p.O;
     float* out = p.logits + (static_cast<long long>(tile_first) * BM + first) * p.O;
+    bool all = true;  // results are finite
     for (int i = threadIdx.x; i < n; i += LG_THREADS) {
       const int r = i / p.O, c = i - r * p.O;
       const uint32_t at = smem_u32(tile_out + (first + r) * p.pitch + c);
@@ -370,7 +430,10 @@ __global__ void __launch_bounds__(LG_THREADS, 1)
       for (int k = 0; k < MAX_CLUSTER; ++k)
         if (k < cs) v += part[k];
       out[i] = v;
+      all &= finite(v);
     }
+    if (__any_sync(0xffffffffu, !all))
+      mend_not_finite(p.src, out, n, threadIdx.x - lane, LG_THREADS, static_cast<long long>(tile_first) * BM + first);
   }
   cluster_sync_all();  // no CTA ends while its sums are read
 }
@@ -415,6 +478,7 @@ cudaError_t launch_fused(const LogitsArgs& a, const Plan& plan, cudaStream_t s) 
   p.b_local = a.b_local;
   p.b_global = a.b_global;
   p.logits = a.logits;
+  p.src = Source{static_cast<const __nv_bfloat16*>(a.X), a.W_local, a.W_global, a.b_local, a.b_global, a.E, plan.O, a.d};
   p.T = a.T;
   p.E = a.E;
   p.O = plan.O;
@@ -488,7 +552,10 @@ cudaError_t launch_gate_logits(const LogitsArgs& a, bool bf16, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   KernelScope ks("logits_sum", s);
   e = launch_kernel(logits_sum_kernel, dim3(static_cast<unsigned>((static_cast<long long>(a.T) * p.O + 255) / 256)), dim3(256), 0,
-                    s, part, p.ranges, bf16 ? 3 : 1, p.N, a.T, a.E, p.O, a.b_local, a.b_global, a.logits);
+                    s, part, p.ranges, bf16 ? 3 : 1, p.N, a.T,
+                    Source{bf16 ? static_cast<const __nv_bfloat16*>(a.X) : nullptr, a.W_local, a.W_global, a.b_local, a.b_global,
+                           a.E, p.O, a.d},
+                    a.logits);
   if (e != cudaSuccess) return e;
   return cudaGetLastError();
 }
