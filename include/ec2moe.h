@@ -340,8 +340,13 @@ ec2moe_status ec2moe_layer_forward_pipelined(const ec2moe_layer_desc* desc, cons
  * for each block of EC2MOE_FP8_BLOCK columns: a stored value q stands for q times
  * its block's scale.  Activations have a scale per row and block
  * ([rows, ceil(cols / 128)]), weights one per 128 x 128 block
- * ([mats, ceil(rows / 128), ceil(cols / 128)]); scales are any fp32 numbers, not
- * only those of ec2moe_fp8_quantize.  Rows are dense and multiples of 16 bytes
+ * ([mats, ceil(rows / 128), ceil(cols / 128)]).  Scales need not be those of
+ * ec2moe_fp8_quantize, but a row's scale and a weight block's are multiplied with each
+ * other in fp32 before a block's sum is multiplied by them: where that product overflows
+ * the result is an infinity or NaN (also of a sum of 0), where it is below 2^-126 it has
+ * lost bits, even if the result itself would be an ordinary number.  (Quantised data
+ * gets there when the largest magnitudes of a row's block and of a weight block multiply
+ * to more than 2^145 or less than 2^-108.)  Rows are dense and multiples of 16 bytes
  * (cols, d, d_ff multiples of 16; others return EC2MOE_ERR_MISALIGNED); a last
  * block may be narrower than 128.  The paper has no counterpart: its experts
  * (Eq. 1) are computed from rounded inputs here, with fp32 sums. */
