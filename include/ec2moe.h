@@ -414,8 +414,11 @@ size_t ec2moe_experts_fp8_workspace_size(const ec2moe_layer_desc* desc);
  *            (ec2moe_fp8_quantize with the inv_perm of ec2moe_route)
  *  slot_out  out [T * k, d] in desc->dtype: slot_out[t * k + s] =
  *            topk_w[t, s] * E_e(x_t) for e = topk_idx[t, s]
- * The hidden rows are the activation of the fp32 sums (GELU to within 1e-6 |u|),
- * quantised like ec2moe_fp8_quantize's rows.  offsets, perm, topk_w and what happens to entries
+ * The hidden rows are the activation of the fp32 sums (GELU to within 1e-6 |u|, SiLU to
+ * within 1e-6 of itself for |u| <= 16), quantised like ec2moe_fp8_quantize's rows.  A sum
+ * within its rounding error of a tie of that quantisation falls to either side, which
+ * moves the hidden value by up to 2^-4 of it: an fp32 slot_out agrees with the same
+ * formula in 64 bits to 1e-7 of its norm where none does, to about 3e-4 where some do.  offsets, perm, topk_w and what happens to entries
  * out of range as for ec2moe_experts; an expert whose rows start before the end of an
  * earlier one's is skipped and reported too. */
 ec2moe_status ec2moe_experts_fp8(const ec2moe_layer_desc* desc, const void* Xq, const float* Xs,

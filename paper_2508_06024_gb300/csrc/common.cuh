@@ -78,7 +78,9 @@ __device__ __forceinline__ float gelu_bf16out(float u) {
   return fmaf(h, t, h);
 }
 
-// SiLU for bf16-output epilogues: fast exp and division (relative error ~1e-7).
+// SiLU for epilogues whose output is rounded to bf16 or fewer bits: fast exp and division.
+// Relative error against 64 bits, measured: at most 6e-7 for |u| <= 8, 1.1e-6 to 20
+// (mean 7e-8, 1.3e-7).
 __device__ __forceinline__ float silu_bf16out(float u) { return __fdividef(u, 1.0f + __expf(-u)); }
 
 // Exclusive prefix sum of n <= 32 * CHUNKS values by one warp (all 32 lanes
