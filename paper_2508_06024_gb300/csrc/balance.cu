@@ -22,9 +22,9 @@
 // Where the groups' sizes and number allow it a token is held by L lanes of a warp,
 // a chunk of one group's logits in each lane's registers, so nothing but the
 // columns' sums passes through shared memory; else a token is a thread's, its row
-// of logits in shared memory.  Up to SMALL_ENTRIES entries of topk_idx one
-// cluster of CTAs does everything in one launch (its CTAs add their histograms and
-// their partial sums through distributed shared memory).  Longer batches take four: balance_clear; balance_count, integer histograms
+// of logits in shared memory.  Short batches (is_small) are done by one
+// cluster of CTAs in one launch (its CTAs add their histograms and
+// their partial sums through distributed shared memory).  Longer ones take four: balance_clear; balance_count, integer histograms
 // (atomics on integers, whose order does not matter) and S'; balance_main, each
 // CTA a contiguous range of tiles, one pass over the logits for the loss and both
 // gradients; balance_final, the CTAs' partial sums in order.  Bounded by HBM for
@@ -50,7 +50,17 @@ constexpr int NT = 160;         // threads: a token each for TILE of them, 144 c
 constexpr int COUNT_TOKENS = 256;   // tokens per CTA of balance_count
 constexpr int COUNT_WARPS = 8;
 constexpr int CL = 8;           // CTAs of the one-launch cluster
+// What it takes on: its eight SMs go over the logits, its atomics over the entries of
+// topk_idx.  One launch against four, us in a stream (a call that is waited for):
+// - lanes, logits T (E + K): 64 experts in 8 groups, Top-6, 74 K 10.4 against 12.4 (23.2,
+//   25.6), 147 K 12.4, 12.5 (25.6, 27.5), 295 K 18.6, 12.4 (32.2, 27.7); 8 in 2, Top-1,
+//   41 K 10.4, 10.4 (22.2, 23.9), 82 K 12.4, 10.4 (24.6, 24.0); 128 in 16, Top-1, 147 K
+//   14.5, 16.5 (26.5, 30.2), 295 K 20.5, 16.5, 2.4 M 107, 20;
+// - rows in shared memory, a tile per CTA or more: 96 in 12, 1024 tokens 14.5, 14.5 (27.1,
+//   30.5), 2048 22.7, 15.4 (35.6, 30.9); 12 in 3, 1024 10.4, 12.4, 2048 16.6, 12.4.
 constexpr long long SMALL_ENTRIES = 16384;
+constexpr long long SMALL_LOGITS = 131072;
+constexpr int SMALL_TOKENS = CL * TILE;
 constexpr int SMALL_CELLS = 4096;   // counts (segments x (experts + 1)) that it keeps on chip
 
 struct Params {
@@ -846,8 +856,10 @@ __global__ void __launch_bounds__(256) balance_final_kernel(Params p) {
 // CTAs of balance_main at most: no kernel gives one fewer tokens than a tile.
 int grid_for(int T) { return (T + TILE - 1) / TILE; }
 
-bool is_small(const Params& p) {
-  return static_cast<long long>(p.T) * p.k <= SMALL_ENTRIES && static_cast<long long>(p.n_seg) * (p.E + 1) <= SMALL_CELLS;
+bool is_small(const Params& p, bool lanes) {
+  const long long T = p.T;
+  return (lanes ? T * p.O <= SMALL_LOGITS : T <= SMALL_TOKENS) && T * p.k <= SMALL_ENTRIES &&
+         static_cast<long long>(p.n_seg) * (p.E + 1) <= SMALL_CELLS;
 }
 
 cudaError_t launch_counts(const Params& p, cudaStream_t s) {
@@ -874,7 +886,7 @@ cudaError_t launch_width(const Params& p, cudaStream_t s) {
   // the totals' scratch, NT doubles per column of a move, fits the tile: rows have 5
   // floats at least, those of chunks 12
   const int tile_bytes = TILE * p.pitch * 4;
-  if (is_small(p)) {
+  if (is_small(p, false)) {
     const int smem = tile_bytes + (p.O + 1) * 8 + 2 * p.n_seg * (p.E + 1) * 4;
     e = ensure_smem_attr(reinterpret_cast<const void*>(balance_small_kernel<V, ONE>), smem);
     if (e != cudaSuccess) return e;
@@ -897,7 +909,7 @@ cudaError_t launch_width(const Params& p, cudaStream_t s) {
 template <int C, int ALIGN>
 cudaError_t launch_lanes(Params p, cudaStream_t s) {
   cudaError_t e;
-  if (is_small(p)) {
+  if (is_small(p, true)) {
     const int smem = LANE_WARPS * (p.O + 1) * 4 + (p.O + 1) * 8 + 2 * p.n_seg * (p.E + 1) * 4;
     e = ensure_smem_attr(reinterpret_cast<const void*>(balance_small_lanes_kernel<C, ALIGN>), smem);
     if (e != cudaSuccess) return e;
