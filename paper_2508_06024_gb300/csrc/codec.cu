@@ -104,6 +104,9 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
   uint64_t* drain = zfull + 3;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(zfull + 4);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  // what the roles leave in flight when they end: the producer's stages (low half) and the
+  // phases that they complete, the lane + 1 of the MMA warp that issued MMAs
+  volatile uint32_t* in_flight = tmem_slot + 2;
   int* s_off = reinterpret_cast<int*>(tmem_slot + 4);  // [E + 1]
 
   const int warp = threadIdx.x >> 5;
@@ -127,6 +130,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
     mbar_init(smem_u32(xfull), 1);
     mbar_init(smem_u32(drain), 1);
     *abort_flag = 0;
+    in_flight[0] = in_flight[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -181,10 +185,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
           phase ^= 1u;
         }
       }
-      if (!ok || *abort_flag) {
-        for (int s = 0; s < C::STAGES; ++s)
-          if (issued & (1u << s)) mbar_drain(smem_u32(&full[s]), (issued_phase >> s) & 1u, DRAIN_CYCLES);
-      }
+      if (lane == 0) in_flight[0] = issued | (issued_phase << 16);
     }
   } else if (warp == 1) {
     // ---------------------------------------------------------------- MMA issuer
@@ -246,10 +247,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
         }
       }
       if (ok && issue) umma_commit(smem_u32(xfull));
-      if ((!ok || *abort_flag) && any && issue) {
-        umma_commit(smem_u32(drain));
-        mbar_drain(smem_u32(drain), 0, DRAIN_CYCLES);
-      }
+      if (any && issue) in_flight[1] = lane + 1;
     }
   } else {
     // ---------------------------------------------------------------- epilogue
@@ -369,6 +367,16 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
 
   tc_fence_before();
   __syncthreads();
+  if (*abort_flag) {  // no warp waits any more: the same in all of them
+    if (warp == 0) {
+      drain_copies(smem_u32(full), in_flight[0] & 0xffffu, in_flight[0] >> 16);
+    } else if (warp == 1 && in_flight[1] == lane + 1u) {
+      // the thread that issued the MMAs: a commit covers its own
+      umma_commit(smem_u32(drain));
+      mbar_drain(smem_u32(drain), 0, DRAIN_CYCLES);
+    }
+    __syncthreads();
+  }
   if (warp == 1) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");

@@ -665,9 +665,8 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
         drain_copies(smem_u32(full), copies & 0xffffu, copies >> 16);
       } else if (copies) {
         // the odd CTA's copies complete on the even one's barriers, which has waited only
-        // for those that it expected: a fixed time
-        const unsigned long long t0 = globaltimer_ns();
-        while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
+        // for those that it expected
+        wait_for_remote_copies();
       }
     } else if (warp == 1 && in_flight[1] == lane + 1u) {
       // the thread that issued the MMAs: a commit covers its own

@@ -431,6 +431,23 @@ __global__ void __launch_bounds__(256) gate_split_kernel(const float* W_local, c
     *reinterpret_cast<U4*>(Wsplit + ((size_t)j * n_pad + o) * d + c) = U4{t[j][0], t[j][1], t[j][2], t[j][3]};
 }
 
+// The end of a CTA of which a wait gave up: its copies and MMAs in flight, and partials
+// whose receiving wait gave up.
+__device__ __noinline__ void abort_end(int thread, const uint32_t* end, int stages, int cs) {
+  using namespace ec2moe::tc;
+  const int warp = thread >> 5, lane = thread & 31;
+  const uint32_t copies = end[1], issuer = end[2], full = end[3], drain = full + (3 * stages + 4) * 8;
+  if (warp == 0) {
+    drain_copies(full, copies & 0xffffu, copies >> 16);
+  } else if (warp == 1 && issuer == lane + 1u) {
+    // the thread that issued the MMAs: a commit covers its own
+    umma_commit(drain);
+    mbar_drain(drain, 0, DRAIN_CYCLES);
+  } else if (cs > 1 && warp == 2 && lane == 0) {
+    wait_for_remote_copies();
+  }
+}
+
 template <int NB, bool PREP>
 __global__ void __launch_bounds__(PREP ? GC_THREADS : GC_THREADS + 32, 1)
     gate_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW,
@@ -461,7 +478,14 @@ __global__ void __launch_bounds__(PREP ? GC_THREADS : GC_THREADS + 32, 1)
   uint64_t* drain = tempty + 2;
   uint64_t* recvb = drain + 1;  // partial logits from the other CTAs of the cluster (cs > 1)
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(recvb + 1);
+  // For the end of the kernel: the address of the abort flag, what the roles leave in flight
+  // (the producer's stages in the low half and the phases that they complete, the lane + 1
+  // of the MMA warp that issued MMAs), the address of the barriers.  At a fixed address:
+  // derived from the others' it took registers that the 72-row form has not (16384 x 2048:
+  // 45.1 us, 43.2 without).
+  __shared__ uint32_t s_end[4];
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  volatile uint32_t* in_flight = s_end + 1;
 
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
@@ -493,6 +517,9 @@ __global__ void __launch_bounds__(PREP ? GC_THREADS : GC_THREADS + 32, 1)
     mbar_init(smem_u32(drain), 1);
     mbar_init(smem_u32(recvb), 1);
     *abort_flag = 0;
+    in_flight[0] = in_flight[1] = 0;
+    s_end[0] = smem_u32(const_cast<int*>(abort_flag));
+    s_end[3] = smem_u32(full);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     // the owned rows' partials of the other cs - 1 CTAs (one tile per cluster)
@@ -588,10 +615,7 @@ __global__ void __launch_bounds__(PREP ? GC_THREADS : GC_THREADS + 32, 1)
           phase ^= 1u;
         }
       }
-      if (!ok || *abort_flag) {
-        for (int s = 0; s < S; ++s)
-          if (issued & (1u << s)) mbar_drain(smem_u32(&full[s]), (issued_phase >> s) & 1u, DRAIN_CYCLES);
-      }
+      if (lane == 0) in_flight[0] = issued | (issued_phase << 16);
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer
@@ -647,10 +671,7 @@ __global__ void __launch_bounds__(PREP ? GC_THREADS : GC_THREADS + 32, 1)
           acc ^= 1;
         }
       }
-      if ((!ok || *abort_flag) && any && issue) {
-        umma_commit(smem_u32(drain));
-        mbar_drain(smem_u32(drain), 0, DRAIN_CYCLES);
-      }
+      if (any && issue) in_flight[1] = lane + 1;
     }
   } else if (!PREP && warp == GC_WARM_WARP) {
     // the decision's code to the SM, as an idle warp does below with prepared rows
@@ -880,6 +901,10 @@ __global__ void __launch_bounds__(PREP ? GC_THREADS : GC_THREADS + 32, 1)
   __syncthreads();
   // no CTA of the cluster leaves while partials to or from it are in flight
   if (cs > 1) cluster_sync_all();
+  if (ld_shared_u32(s_end[0])) {  // no warp waits any more: the same in all of them
+    abort_end(threadIdx.x, s_end, gp.stages, cs);
+    __syncthreads();
+  }
   if (warp == 1) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");
@@ -889,7 +914,7 @@ __global__ void __launch_bounds__(PREP ? GC_THREADS : GC_THREADS + 32, 1)
 // Stages that fit next to the logits, routing tables and received partials.
 int gc_stages(int O, int k, int E, int cs, bool raw) {
   for (int s = GC_MAX_STAGES; s >= 2; --s)
-    if (GcLayout(O, k, E, s, cs, raw).total + 1024 <= 232448) return s;
+    if (GcLayout(O, k, E, s, cs, raw).total + 1024 + 16 <= 232448) return s;  // 16: static
   return 0;
 }
 
@@ -907,7 +932,7 @@ int gc_cluster_size(int O, int k, int E, int d) {
     return v && atoi(v) > 0 ? atoi(v) : GC_SPLIT_MIN_NK;
   }();
   if ((d + GC_BK - 1) / GC_BK < min_nk) return 1;
-  return GcLayout(O, k, E, 4, GC_CS, true).warm_off + 1024 <= 232448 ? GC_CS : 1;
+  return GcLayout(O, k, E, 4, GC_CS, true).warm_off + 1024 + 16 <= 232448 ? GC_CS : 1;
 }
 
 // CTAs the gate kernel launches (cs > 1: a cluster per tile, run in waves

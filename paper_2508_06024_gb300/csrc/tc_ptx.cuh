@@ -92,6 +92,13 @@ __device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity, long l
   }
 }
 
+// A word that other warps write without a barrier in between.
+__device__ __forceinline__ uint32_t ld_shared_u32(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+
 // What a CTA has in flight when one of its waits gave up.  Any of its warps can be the
 // one that gives up, after the producer and the MMA issuer have issued their last, so
 // this is asked once all warps have ended their roles (a __syncthreads after them) and
@@ -252,6 +259,13 @@ __device__ __forceinline__ unsigned long long globaltimer_ns() {
   unsigned long long t;
   asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
   return t;
+}
+
+// After an abort: a fixed time in which copies that complete on another CTA's barriers,
+// or that another CTA sends here, land.
+__device__ __forceinline__ void wait_for_remote_copies() {
+  const unsigned long long t0 = globaltimer_ns();
+  while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
 }
 
 // ------------------------------------------------------------------ CTA pairs (cluster of 2, cta_group::2)

@@ -56,8 +56,8 @@ constexpr int SW_STAGE_BYTES = SW_W_BYTES + SW_X_BYTES;
 constexpr int SW_OFF_X = SW_STAGES * SW_W_BYTES;
 constexpr int SW_OFF_BARS = SW_OFF_X + SW_STAGES * SW_X_BYTES;
 constexpr int SW_N_BARS = 2 * SW_STAGES + 2 * SW_ACC + 1;
-constexpr int SW_OFF_SLOT = SW_OFF_BARS + SW_N_BARS * 8;  // TMEM address, abort flag, active-group count
-constexpr int SW_OFF_LIST = SW_OFF_SLOT + 16;             // per active group: id, first row, rows
+constexpr int SW_OFF_SLOT = SW_OFF_BARS + SW_N_BARS * 8;  // TMEM address, abort flag, active-group count, in flight (2)
+constexpr int SW_OFF_LIST = SW_OFF_SLOT + 32;             // per active group: id, first row, rows
 constexpr int SW_OFF_XCH = (SW_OFF_LIST + 3 * SW_MAX_GROUPS * 4 + 15) & ~15;
 constexpr int SW_SMEM = SW_OFF_XCH + 64 * SW_XCH_PITCH * 4 + 1024;  // + alignment slack
 static_assert(SW_OFF_X % 1024 == 0 && SW_OFF_BARS % 8 == 0 && SW_OFF_XCH % 16 == 0, "shared layout alignment");
@@ -107,6 +107,9 @@ __global__ void __launch_bounds__(SW_THREADS, 1)
   uint64_t* drain = tempty + SW_ACC;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + SW_OFF_SLOT);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  // what the roles leave in flight when they end: the producer's stages (low half) and the
+  // phases that they complete, the lane + 1 of the MMA warp that issued MMAs
+  volatile uint32_t* in_flight = tmem_slot + 3;
   int* n_active = reinterpret_cast<int*>(tmem_slot + 2);
   int* g_id = reinterpret_cast<int*>(smem + SW_OFF_LIST);
   int* g_r0 = g_id + SW_MAX_GROUPS;
@@ -128,6 +131,7 @@ __global__ void __launch_bounds__(SW_THREADS, 1)
     }
     mbar_init(smem_u32(drain), 1);
     *abort_flag = 0;
+    in_flight[0] = in_flight[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -233,11 +237,7 @@ __global__ void __launch_bounds__(SW_THREADS, 1)
           }
         }
       }
-      if (!ok || *abort_flag) {
-        // Let every copy this CTA started land before shared memory is released.
-        for (int s = 0; s < SW_STAGES; ++s)
-          if (issued & (1u << s)) mbar_drain(smem_u32(&full[s]), (issued_phase >> s) & 1u, DRAIN_CYCLES);
-      }
+      if (lane == 0) in_flight[0] = issued | (issued_phase << 16);
     }
   } else if (warp == 1) {
     {
@@ -291,11 +291,7 @@ __global__ void __launch_bounds__(SW_THREADS, 1)
         if (!ok) break;
         if (issue) umma_commit(smem_u32(&tfull[acc]));
       }
-      if ((!ok || *abort_flag) && any && issue) {
-        // All MMAs issued so far must finish before TMEM is freed.
-        umma_commit(smem_u32(drain));
-        mbar_drain(smem_u32(drain), 0, DRAIN_CYCLES);
-      }
+      if (any && issue) in_flight[1] = lane + 1;
     }
   } else {
     // ---------------------------------------------------------------- epilogue
@@ -378,6 +374,16 @@ __global__ void __launch_bounds__(SW_THREADS, 1)
 
   tc_fence_before();
   __syncthreads();
+  if (*abort_flag) {  // no warp waits any more: the same in all of them
+    if (warp == 0) {
+      drain_copies(smem_u32(full), in_flight[0] & 0xffffu, in_flight[0] >> 16);
+    } else if (warp == 1 && in_flight[1] == lane + 1u) {
+      // the thread that issued the MMAs: a commit covers its own
+      umma_commit(smem_u32(drain));
+      mbar_drain(smem_u32(drain), 0, DRAIN_CYCLES);
+    }
+    __syncthreads();
+  }
   if (warp == 1) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(SW_TMEM_COLS)

@@ -162,6 +162,9 @@ __global__ void __launch_bounds__(TG_THREADS, 1)
   uint64_t* drain = tempty + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + TG_OFF_SLOT);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  // what the roles leave in flight when they end: the producer's stages (low half) and the
+  // phases that they complete, the lane + 1 of the MMA warp that issued MMAs
+  volatile uint32_t* in_flight = tmem_slot + 2;
   int* tile_prefix = reinterpret_cast<int*>(smem + TG_OFF_PREFIX);
   TgGroup* groups = reinterpret_cast<TgGroup*>(smem + TG_OFF_GROUPS);
 
@@ -184,6 +187,7 @@ __global__ void __launch_bounds__(TG_THREADS, 1)
     }
     mbar_init(smem_u32(drain), 1);
     *abort_flag = 0;
+    in_flight[0] = in_flight[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -289,19 +293,7 @@ __global__ void __launch_bounds__(TG_THREADS, 1)
           }
         }
       }
-      if (!ok || *abort_flag) {
-        // Let every copy this CTA started land before shared memory is released.
-        if (rank != 0) {
-          // its copies complete on the even CTA's barriers: wait a fixed time
-          if (issued) {
-            const unsigned long long t0 = globaltimer_ns();
-            while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
-          }
-        } else {
-          for (int s = 0; s < TG_STAGES; ++s)
-            if (issued & (1u << s)) mbar_drain(smem_u32(&full[s]), (issued_phase >> s) & 1u, DRAIN_CYCLES);
-        }
-      }
+      if (lane == 0) in_flight[0] = issued | (issued_phase << 16);
     }
   } else if (warp == 1) {
     if (rank == 0) {
@@ -346,11 +338,7 @@ __global__ void __launch_bounds__(TG_THREADS, 1)
         if (leader) umma_commit_pair_mc(smem_u32(&tfull[used & 1]));
         ++used;
       }
-      if ((!ok || *abort_flag) && any && leader) {
-        // All MMAs issued so far must finish before TMEM is freed.
-        umma_commit_pair(smem_u32(drain));
-        mbar_drain(smem_u32(drain), 0, DRAIN_CYCLES);
-      }
+      if (any && leader) in_flight[1] = lane + 1;
     }
   } else {
     // ---------------------------------------------------------------- epilogue
@@ -462,9 +450,26 @@ __global__ void __launch_bounds__(TG_THREADS, 1)
 
   tc_fence_before();
   __syncthreads();
-  // the even CTA's MMAs write both CTAs' TMEM; neither releases its columns
-  // before both are done with them
+  // the even CTA's MMAs read both CTAs' shared memory and write both CTAs' TMEM; neither
+  // is released before both CTAs are done with them, nor, where a wait of either gave up,
+  // before what is in flight has ended
+  if (threadIdx.x == 0) abort_pair(abort_flag, rank);
+  __syncwarp();
   cluster_sync_all();
+  if (*abort_flag) {  // no warp waits any more: the same in all of them, and in the pair
+    if (warp == 0) {
+      const uint32_t copies = in_flight[0];
+      if (rank == 0) drain_copies(smem_u32(full), copies & 0xffffu, copies >> 16);
+      else if (copies) wait_for_remote_copies();
+    } else if (warp == 1 && in_flight[1] == lane + 1u) {
+      // the thread that issued the MMAs: a commit covers its own
+      umma_commit_pair(smem_u32(drain));
+      mbar_drain(smem_u32(drain), 0, DRAIN_CYCLES);
+    }
+    __syncthreads();
+    __syncwarp();
+    cluster_sync_all();
+  }
   if (warp == 1) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");
