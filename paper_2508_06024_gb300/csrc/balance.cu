@@ -25,9 +25,9 @@
 // of logits in shared memory.  Short batches (is_small) are done by one
 // cluster of CTAs in one launch (its CTAs add their histograms and
 // their partial sums through distributed shared memory).  Longer ones take four: balance_clear; balance_count, integer histograms
-// (atomics on integers, whose order does not matter) and S'; balance_main, each
-// CTA a contiguous range of tiles, one pass over the logits for the loss and both
-// gradients; balance_final, the CTAs' partial sums in order.  Bounded by HBM for
+// (atomics on integers, whose order does not matter) and S'; balance_main or
+// balance_lanes, each CTA a contiguous range of tokens, one pass over the logits for the
+// loss and both gradients; balance_final, the CTAs' partial sums in order.  Bounded by HBM for
 // long batches (the logits are read once, their gradients written once), by the
 // launches for short ones.  Measured: 1021 tokens of 16 experts 8.2 us; 262144 of 64
 // in 64 segments, 158 MB, 45 us, of which main 31 (floor 23).
@@ -607,8 +607,8 @@ __device__ __forceinline__ void cta_totals(const Params& p, const Mover<V>& mv, 
   }
 }
 
-// One tile per CTA: the scheduler evens out what CTAs with several tiles each did
-// not (2048 tiles on 608 CTAs of 3 or 4).
+// One tile per CTA: several each would leave the last of them uneven.  Serves groups of
+// fewer than four experts, and where their size or number is not a power of two.
 template <int V, bool ONE>
 __global__ void __launch_bounds__(NT) balance_main_kernel(Params p) {
   constexpr int M = V < 4 ? V : 4;

@@ -39,7 +39,7 @@
 // What bounds it: a K block of a 128 x 256 tile takes the MMAs 512 clocks, the fp32
 // multiply-adds of its sums 256 and reading them about as long; with the waits and
 // hand-overs between (two buffers, a warp's registers full of sums) a block takes
-// about 930.  16384 x 14336 x 4096 in 8 groups: 780 us = 2.47 PFLOP/s (a library's
+// about 930: no unit is full, what is left is latency.  16384 x 14336 x 4096 in 8 groups: 780 us = 2.47 PFLOP/s (a library's
 // product without scales 509 us), 850 us once power holds the clocks; experts of
 // 14336 x 4096, 1024 tokens: the tensor pipe is busy 50% of the time.
 //
