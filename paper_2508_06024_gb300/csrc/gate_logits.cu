@@ -63,12 +63,26 @@ struct Source {
 __device__ __noinline__ void mend_not_finite(const Source& src, float* out, long long n, long long first, int step,
                                              long long t0) {
   const int lane = threadIdx.x & 31;
+  long long row = -1;  // the token asked for last
+  bool row_nan = false;
   for (long long i0 = first; i0 < n; i0 += step) {
     uint32_t m = __ballot_sync(0xffffffffu, i0 + lane < n && !finite(out[i0 + lane]));
     for (; m; m &= m - 1) {
       const long long i = i0 + __ffs(m) - 1, t = t0 + i / src.O;
       const int o = static_cast<int>(i % src.O);
       const __nv_bfloat16* x = src.X + t * src.d;
+      if (t != row) {
+        bool nan = false;
+        for (int c = 8 * lane; c < src.d; c += 256) {
+          float v[8];
+          load8(x + c, v);
+#pragma unroll
+          for (int u = 0; u < 8; ++u) nan |= isnan(v[u]);
+        }
+        row = t;
+        row_nan = __any_sync(0xffffffffu, nan);
+      }
+      if (row_nan) continue;  // so are its logits, as they stand
       const float* w = gate_row(src.W_local, src.W_global, src.E, src.d, o);
       double s = 0.0;
       for (int c = 4 * lane; c < src.d; c += 128) {
