@@ -483,6 +483,117 @@ ec2moe_status ec2moe_balance_loss(const ec2moe_layer_desc* desc, const float* lo
                                   float* loss, int32_t* counts, float* d_logits, float* d_bias, void* workspace,
                                   size_t ws_bytes, ec2moe_stream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * The norm in front of a layer and what its experts are trained with.  The paper
+ * is about inference and has no counterpart of these; they are the formulas given
+ * here. */
+
+/* The residual's addition and the root-mean-square norm of the sum, row by row:
+ *   h = x + residual,  rstd = 1 / sqrt(mean h^2 + eps),  y = h * rstd * weight
+ * in fp32; y is taken from the sum before it is rounded to H's type.
+ *  dtype, y_dtype  ec2moe_dtype of X, residual and H; of Y
+ *  X, residual     [rows, cols], rows of pitch ld >= cols elements (a multiple of 16
+ *                  bytes); residual NULL: none
+ *  weight          fp32 [cols], or NULL: ones
+ *  eps             finite, >= 0
+ *  H               out, dense, or NULL: h; may be X or residual itself where ld = cols
+ *  rstd            out fp32 [rows], or NULL (ec2moe_rmsnorm_backward needs it)
+ *  Y               out, dense, or NULL
+ *  Q, scale        out, or both NULL: y as ec2moe_fp8_quantize stores rows (block_rows =
+ *                  1), from the fp32 y: e4m3 [rows, cols], dense, and fp32 [rows,
+ *                  ceil(cols / 128)]; what ec2moe_fp8_gemm and ec2moe_experts_fp8 take
+ * One output at least.  cols is a multiple of 8 (with Q of 16), at most 16384 (more
+ * return EC2MOE_ERR_UNSUPPORTED).  The squares are summed in fp32: where that sum
+ * overflows y is 0, as it is for a row with an infinity, whose infinite elements become NaN;
+ * a NaN makes its row NaN.  No rows is a no-op. */
+ec2moe_status ec2moe_rmsnorm(int32_t dtype, int32_t y_dtype, int32_t rows, int32_t cols, int64_t ld, const void* X,
+                             const void* residual, const float* weight, float eps, void* H, float* rstd, void* Y,
+                             void* Q, float* scale, ec2moe_stream_t stream);
+
+/* Bytes of device workspace ec2moe_rmsnorm_backward needs for d_weight on the current
+ * device (0: none, or an invalid size). */
+size_t ec2moe_rmsnorm_backward_workspace_size(int32_t rows, int32_t cols);
+
+/* The gradient of ec2moe_rmsnorm.  With g = dY * weight and xhat = H * rstd:
+ *   dX = rstd * (g - xhat * mean(g * xhat)) + dH,  d_weight = sum over rows of dY * xhat
+ *  dY        y_dtype [rows, cols] of pitch ld >= cols elements
+ *  H, rstd   dense, as ec2moe_rmsnorm wrote them (without a residual H is its X)
+ *  dH        dtype, dense, or NULL: the gradient that arrives at H itself (the residual
+ *            stream behind the norm)
+ *  dX        out, dtype, dense: the gradient of X and of residual; may be dH, H or (of
+ *            the same type, ld = cols) dY itself
+ *  d_weight  out fp32 [cols], or NULL (no workspace then)
+ * The sums are in a fixed order: the same inputs give the same bits.  No rows: d_weight
+ * is 0. */
+ec2moe_status ec2moe_rmsnorm_backward(int32_t dtype, int32_t y_dtype, int32_t rows, int32_t cols, int64_t ld,
+                                      const void* dY, const void* H, const float* rstd, const float* weight,
+                                      const void* dH, void* dX, float* d_weight, void* workspace, size_t ws_bytes,
+                                      ec2moe_stream_t stream);
+
+/* The experts' activation of rows in expert order, with each row's gate weight:
+ *   H[p] = row_scale[perm[p]] * a[p],  a = SiLU(U) * V  or  GELU(U)  (exact erf form)
+ *  U, V       [rows, cols] (dtype), both of pitch ld >= cols elements, so that they may be
+ *             the halves of one matrix (rows of W1 and W3 joined); V for EC2MOE_SWIGLU
+ *  perm       device int32 [rows] (ec2moe_route), or NULL: perm[p] = p
+ *  row_scale  fp32 [rows] (topk_w of ec2moe_gate), or NULL: 1
+ *  H          out [rows, cols], dense
+ * (Eq. 1's factor G(x)_i, applied before the linear down projection instead of behind
+ * it.)  cols is a multiple of 8.  A perm entry outside [0, rows) leaves its row as it
+ * was and ec2moe_last_device_error then reports EC2MOE_ERR_INVALID_ARG.  No rows is a
+ * no-op. */
+ec2moe_status ec2moe_activation(int32_t dtype, int32_t act, int32_t rows, int32_t cols, int64_t ld, const void* U,
+                                const void* V, const int32_t* perm, const float* row_scale, void* H,
+                                ec2moe_stream_t stream);
+
+/* Its gradient, with s = row_scale[perm[p]]:
+ *   dU = s dH da/dU,  dV = s dH SiLU(U),  d_row_scale[perm[p]] = sum over columns of dH * a
+ *  dH           [rows, cols], dense
+ *  dU, dV       out, pitch ld; may be U and V themselves
+ *  H            out, dense, or NULL: the forward's H again (the weights' gradient needs
+ *               it); may be dH itself
+ *  d_row_scale  out fp32 [rows], or NULL
+ * Rows with a perm entry out of range are skipped and reported as above. */
+ec2moe_status ec2moe_activation_backward(int32_t dtype, int32_t act, int32_t rows, int32_t cols, int64_t ld,
+                                         const void* U, const void* V, const int32_t* perm, const float* row_scale,
+                                         const void* dH, void* dU, void* dV, void* H, float* d_row_scale,
+                                         ec2moe_stream_t stream);
+
+/* Bytes of device workspace that any of the three products below needs on the current
+ * device (0: none, or an invalid size): partial results of sums that are cut into ranges
+ * where a call has few tiles. */
+size_t ec2moe_grouped_gemm_workspace_size(int32_t n_groups, int32_t rows, int32_t N, int32_t K);
+
+/* Products grouped by expert of bf16 operands, group g owning the rows [offsets[g],
+ * offsets[g + 1]) of the row matrices and the weights B[g] [N, K] (dense):
+ *   ec2moe_grouped_gemm        C_g  = A_g B_g^T     A [rows, K]   -> C [rows, N]
+ *   ec2moe_grouped_gemm_dgrad  dA_g = dC_g B_g      dC [rows, N]  -> dA [rows, K]
+ *   ec2moe_grouped_gemm_wgrad  dB_g = dC_g^T A_g    dC, A         -> dB [n_groups, N, K]
+ *  offsets     device int32 [n_groups + 1], or NULL with n_groups = 1: all rows
+ *  lda, lddc   row pitches in elements (multiples of 8)
+ *  perm        device int32 [rows] or NULL: row p of the result is written to row perm[p]
+ *              of C or dA (the token's slot: ec2moe_combine then adds them up); the
+ *              destinations of different rows differ
+ *  out_dtype   EC2MOE_BF16 or EC2MOE_F32: type of the result, rows of pitch ldc or ldda
+ *              elements (a multiple of 16 bytes); dB is dense
+ *  accumulate  1: dB is added to (EC2MOE_F32 only)
+ * N and K are multiples of 8.  Sums are in fp32, rounded once to the result; the same
+ * inputs give the same bits.  Rows of no group are not written and take no part, whatever
+ * they hold; a group without rows has dB = 0 (accumulate: as it was).  A group whose
+ * range is not inside [0, rows], or which starts before the end of a group before it,
+ * counts as one without rows, and a destination outside [0, rows) is skipped;
+ * ec2moe_last_device_error then reports EC2MOE_ERR_INVALID_ARG. */
+ec2moe_status ec2moe_grouped_gemm(int32_t n_groups, int32_t rows, int32_t N, int32_t K, const void* A, int64_t lda,
+                                  const int32_t* offsets, const void* B, const int32_t* perm, int32_t out_dtype, void* C,
+                                  int64_t ldc, void* workspace, size_t ws_bytes, ec2moe_stream_t stream);
+ec2moe_status ec2moe_grouped_gemm_dgrad(int32_t n_groups, int32_t rows, int32_t N, int32_t K, const void* dC, int64_t lddc,
+                                        const int32_t* offsets, const void* B, const int32_t* perm, int32_t out_dtype,
+                                        void* dA, int64_t ldda, void* workspace, size_t ws_bytes,
+                                        ec2moe_stream_t stream);
+ec2moe_status ec2moe_grouped_gemm_wgrad(int32_t n_groups, int32_t rows, int32_t N, int32_t K, const void* dC, int64_t lddc,
+                                        const void* A, int64_t lda, const int32_t* offsets, int32_t out_dtype,
+                                        int32_t accumulate, void* dB, void* workspace, size_t ws_bytes,
+                                        ec2moe_stream_t stream);
+
 /* Number of kernels the last successful call on this host thread enqueued. */
 int32_t ec2moe_last_launch_count(void);
 
@@ -495,7 +606,9 @@ int32_t ec2moe_last_launch_count(void);
  * "shared_down", "ffn_up", "ffn_down" (routed and shared experts in one launch),
  * "combine", "sum_counts", "quantize_rows", "quantize_blocks", "fp8_gemm", "fp8_up",
  * "fp8_down", "fp8_sum", "logits_prep", "logits_gemm", "logits_sum", "balance",
- * "balance_clear", "balance_count", "balance_main", "balance_final"); `ms` its device
+ * "balance_clear", "balance_count", "balance_main", "balance_final", "rmsnorm",
+ * "rmsnorm_backward", "rmsnorm_dweight", "activation", "activation_backward",
+ * "grouped_gemm", "grouped_dgrad", "grouped_wgrad", "grouped_join"); `ms` its device
  * duration.  Profiling is off by default and costs nothing when off. */
 ec2moe_status ec2moe_profile_enable(int32_t enable);
 /* Restricts profiling to one launch per call: with launch_index >= 0 only the

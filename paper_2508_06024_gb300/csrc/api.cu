@@ -5,6 +5,7 @@
 
 #include <stdlib.h>
 
+#include <cmath>
 #include <mutex>
 #include <vector>
 
@@ -610,6 +611,39 @@ Fp8Ws fp8_ws(const ec2moe_layer_desc* d) {
   const size_t down = fp8_swap_bytes(d->E, (int)rows, d->d, d->d_ff, 1);
   w.total = w.part + align_up(up > down ? up : down);
   return w;
+}
+
+// Norm and activation: sizes that the kernels' registers and 16-byte rows take.
+bool known_dtype(int dtype) { return dtype == EC2MOE_F32 || dtype == EC2MOE_BF16; }
+ec2moe_status check_rows(int dtype, int rows, int cols, int64_t ld) {
+  if (!known_dtype(dtype) || rows < 0 || cols <= 0 || ld < cols) return EC2MOE_ERR_INVALID_ARG;
+  if (cols % 8 != 0 || ld % (dtype == EC2MOE_BF16 ? 8 : 4) != 0) return EC2MOE_ERR_MISALIGNED;
+  return EC2MOE_OK;
+}
+
+// Grouped bf16 products: sizes that 32-bit indexes and 16-byte rows take.
+ec2moe_status check_grouped(int n_groups, int rows, int N, int K) {
+  if (n_groups <= 0 || rows < 0 || N <= 0 || K <= 0) return EC2MOE_ERR_INVALID_ARG;
+  if (n_groups > EC2MOE_MAX_EXPERTS) return EC2MOE_ERR_UNSUPPORTED;
+  if (N % 8 != 0 || K % 8 != 0) return EC2MOE_ERR_MISALIGNED;
+  // indexes are 32-bit up to the end of the last tile, of 256 rows or columns
+  constexpr int most = 0x7fffffff - 255;
+  if (rows > most || N > most || K > most) return EC2MOE_ERR_UNSUPPORTED;
+  // units: tiles of 256 x 128, a partial one per group, times the ranges of a split sum
+  const long long nb = ((long long)N + 127) / 128, kb = ((long long)K + 127) / 128;
+  const long long wide = nb > kb ? nb : kb, units = 0x7fffffffLL / GROUPED_MAX_SPLIT;
+  if (nb * kb > units / n_groups || ((long long)rows / 256 + n_groups) * wide > units) return EC2MOE_ERR_UNSUPPORTED;
+  return EC2MOE_OK;
+}
+
+ec2moe_status run_grouped(GroupedArgs& g, int form, int out_dtype, void* workspace, size_t ws_bytes, cudaStream_t s) {
+  const size_t need = grouped_bytes(form, g.G, g.rows, g.N, g.K);
+  if (need > 0 && (!workspace || ws_bytes < need)) return EC2MOE_ERR_WORKSPACE;
+  if (need > 0 && !aligned16(workspace)) return EC2MOE_ERR_MISALIGNED;
+  g.out_bf16 = out_dtype == EC2MOE_BF16;
+  g.workspace = workspace;
+  g.timeout_cycles = default_timeout_cycles();
+  return launch_grouped(g, form, s) == cudaSuccess ? EC2MOE_OK : EC2MOE_ERR_CUDA;
 }
 
 // Argument checks of a whole-layer call (everything but the workspace).
@@ -1343,10 +1377,176 @@ ec2moe_status ec2moe_balance_loss(const ec2moe_layer_desc* desc, const float* lo
   return EC2MOE_OK;
 }
 
+// ------------------------------------------- norm, activation, grouped products
+ec2moe_status ec2moe_rmsnorm(int32_t dtype, int32_t y_dtype, int32_t rows, int32_t cols, int64_t ld, const void* X,
+                             const void* residual, const float* weight, float eps, void* H, float* rstd, void* Y,
+                             void* Q, float* scale, ec2moe_stream_t stream) {
+  reset_launch_count();
+  ec2moe_status st = check_rows(dtype, rows, cols, ld);
+  if (st != EC2MOE_OK) return st;
+  if (!known_dtype(y_dtype) || !(eps >= 0.0f) || std::isinf(eps)) return EC2MOE_ERR_INVALID_ARG;
+  if ((Q != nullptr) != (scale != nullptr) || (!H && !rstd && !Y && !Q)) return EC2MOE_ERR_INVALID_ARG;
+  if (Q && cols % 16 != 0) return EC2MOE_ERR_MISALIGNED;
+  if (cols > NORM_MAX_COLS) return EC2MOE_ERR_UNSUPPORTED;
+  if (rows == 0) return EC2MOE_OK;
+  EC2MOE_REQUIRE_PTR(X);
+  if (!aligned16(residual) || !aligned16(weight) || !aligned16(H) || !aligned16(Y) || !aligned16(Q))
+    return EC2MOE_ERR_MISALIGNED;
+  const NormArgs a{X, residual, weight, ld, rows, cols, eps, H, rstd, Y, Q, scale};
+  EC2MOE_CUDA(launch_rmsnorm(a, dtype == EC2MOE_BF16, y_dtype == EC2MOE_BF16, stream));
+  return EC2MOE_OK;
+}
+
+size_t ec2moe_rmsnorm_backward_workspace_size(int32_t rows, int32_t cols) {
+  if (rows <= 0 || cols <= 0 || cols % 8 != 0 || cols > NORM_MAX_COLS) return 0;
+  return align_up(norm_backward_bytes(rows, cols));
+}
+
+ec2moe_status ec2moe_rmsnorm_backward(int32_t dtype, int32_t y_dtype, int32_t rows, int32_t cols, int64_t ld,
+                                      const void* dY, const void* H, const float* rstd, const float* weight,
+                                      const void* dH, void* dX, float* d_weight, void* workspace, size_t ws_bytes,
+                                      ec2moe_stream_t stream) {
+  reset_launch_count();
+  ec2moe_status st = check_rows(dtype, rows, cols, cols);
+  if (st != EC2MOE_OK) return st;
+  st = check_rows(y_dtype, rows, cols, ld);
+  if (st != EC2MOE_OK) return st;
+  if (cols > NORM_MAX_COLS) return EC2MOE_ERR_UNSUPPORTED;
+  if (!aligned16(weight) || !aligned16(dH) || !aligned16(d_weight)) return EC2MOE_ERR_MISALIGNED;
+  if (rows == 0) {
+    if (d_weight) EC2MOE_CUDA(cudaMemsetAsync(d_weight, 0, static_cast<size_t>(cols) * 4, stream));
+    return EC2MOE_OK;
+  }
+  EC2MOE_REQUIRE_PTR(dY);
+  EC2MOE_REQUIRE_PTR(H);
+  EC2MOE_REQUIRE_PTR(dX);
+  if (!rstd) return EC2MOE_ERR_INVALID_ARG;
+  if (d_weight && (!workspace || ws_bytes < ec2moe_rmsnorm_backward_workspace_size(rows, cols))) return EC2MOE_ERR_WORKSPACE;
+  if (d_weight && !aligned16(workspace)) return EC2MOE_ERR_MISALIGNED;
+  const NormBackArgs a{dY, H, rstd, weight, dH, ld, rows, cols, dX, d_weight, static_cast<float*>(workspace)};
+  EC2MOE_CUDA(launch_rmsnorm_backward(a, dtype == EC2MOE_BF16, y_dtype == EC2MOE_BF16, stream));
+  return EC2MOE_OK;
+}
+
+ec2moe_status ec2moe_activation(int32_t dtype, int32_t act, int32_t rows, int32_t cols, int64_t ld, const void* U,
+                                const void* V, const int32_t* perm, const float* row_scale, void* H,
+                                ec2moe_stream_t stream) {
+  reset_launch_count();
+  ec2moe_status st = check_rows(dtype, rows, cols, ld);
+  if (st != EC2MOE_OK) return st;
+  if (act != EC2MOE_GELU && act != EC2MOE_SWIGLU) return EC2MOE_ERR_INVALID_ARG;
+  if (rows == 0) return EC2MOE_OK;
+  EC2MOE_REQUIRE_PTR(U);
+  EC2MOE_REQUIRE_PTR(H);
+  if (act == EC2MOE_SWIGLU) EC2MOE_REQUIRE_PTR(V);
+  ActArgs a{};
+  a.U = U;
+  a.V = V;
+  a.ld = ld;
+  a.rows = rows;
+  a.cols = cols;
+  a.perm = perm;
+  a.row_scale = row_scale;
+  a.H = H;
+  EC2MOE_CUDA(launch_activation(a, dtype == EC2MOE_BF16, act == EC2MOE_SWIGLU, false, stream));
+  return EC2MOE_OK;
+}
+
+ec2moe_status ec2moe_activation_backward(int32_t dtype, int32_t act, int32_t rows, int32_t cols, int64_t ld,
+                                         const void* U, const void* V, const int32_t* perm, const float* row_scale,
+                                         const void* dH, void* dU, void* dV, void* H, float* d_row_scale,
+                                         ec2moe_stream_t stream) {
+  reset_launch_count();
+  ec2moe_status st = check_rows(dtype, rows, cols, ld);
+  if (st != EC2MOE_OK) return st;
+  if (act != EC2MOE_GELU && act != EC2MOE_SWIGLU) return EC2MOE_ERR_INVALID_ARG;
+  if (rows == 0) return EC2MOE_OK;
+  EC2MOE_REQUIRE_PTR(U);
+  EC2MOE_REQUIRE_PTR(dH);
+  EC2MOE_REQUIRE_PTR(dU);
+  if (act == EC2MOE_SWIGLU) {
+    EC2MOE_REQUIRE_PTR(V);
+    EC2MOE_REQUIRE_PTR(dV);
+  }
+  if (!aligned16(H)) return EC2MOE_ERR_MISALIGNED;
+  const ActArgs a{U, V, ld, rows, cols, perm, row_scale, dH, dU, dV, H, d_row_scale};
+  EC2MOE_CUDA(launch_activation(a, dtype == EC2MOE_BF16, act == EC2MOE_SWIGLU, true, stream));
+  return EC2MOE_OK;
+}
+
+size_t ec2moe_grouped_gemm_workspace_size(int32_t n_groups, int32_t rows, int32_t N, int32_t K) {
+  if (check_grouped(n_groups, rows, N, K) != EC2MOE_OK || rows == 0) return 0;
+  size_t most = 0;
+  for (int form : {GROUPED_FWD, GROUPED_DGRAD, GROUPED_WGRAD}) {
+    const size_t b = grouped_bytes(form, n_groups, rows, N, K);
+    most = b > most ? b : most;
+  }
+  return align_up(most);
+}
+
+ec2moe_status ec2moe_grouped_gemm(int32_t n_groups, int32_t rows, int32_t N, int32_t K, const void* A, int64_t lda,
+                                  const int32_t* offsets, const void* B, const int32_t* perm, int32_t out_dtype, void* C,
+                                  int64_t ldc, void* workspace, size_t ws_bytes, ec2moe_stream_t stream) {
+  reset_launch_count();
+  ec2moe_status st = check_grouped(n_groups, rows, N, K);
+  if (st != EC2MOE_OK) return st;
+  if (!known_dtype(out_dtype) || lda < K || ldc < N || (!offsets && n_groups != 1)) return EC2MOE_ERR_INVALID_ARG;
+  if (lda % 8 != 0 || ldc % (out_dtype == EC2MOE_BF16 ? 8 : 4) != 0) return EC2MOE_ERR_MISALIGNED;
+  if (rows == 0) return EC2MOE_OK;
+  EC2MOE_REQUIRE_PTR(A);
+  EC2MOE_REQUIRE_PTR(B);
+  EC2MOE_REQUIRE_PTR(C);
+  GroupedArgs g{A, lda, B, K, offsets, perm, n_groups, rows, N, K, C, ldc};
+  g.name = "grouped_gemm";
+  return run_grouped(g, GROUPED_FWD, out_dtype, workspace, ws_bytes, stream);
+}
+
+ec2moe_status ec2moe_grouped_gemm_dgrad(int32_t n_groups, int32_t rows, int32_t N, int32_t K, const void* dC, int64_t lddc,
+                                        const int32_t* offsets, const void* B, const int32_t* perm, int32_t out_dtype,
+                                        void* dA, int64_t ldda, void* workspace, size_t ws_bytes,
+                                        ec2moe_stream_t stream) {
+  reset_launch_count();
+  ec2moe_status st = check_grouped(n_groups, rows, N, K);
+  if (st != EC2MOE_OK) return st;
+  if (!known_dtype(out_dtype) || lddc < N || ldda < K || (!offsets && n_groups != 1)) return EC2MOE_ERR_INVALID_ARG;
+  if (lddc % 8 != 0 || ldda % (out_dtype == EC2MOE_BF16 ? 8 : 4) != 0) return EC2MOE_ERR_MISALIGNED;
+  if (rows == 0) return EC2MOE_OK;
+  EC2MOE_REQUIRE_PTR(dC);
+  EC2MOE_REQUIRE_PTR(B);
+  EC2MOE_REQUIRE_PTR(dA);
+  GroupedArgs g{dC, lddc, B, K, offsets, perm, n_groups, rows, N, K, dA, ldda};
+  g.name = "grouped_dgrad";
+  return run_grouped(g, GROUPED_DGRAD, out_dtype, workspace, ws_bytes, stream);
+}
+
+ec2moe_status ec2moe_grouped_gemm_wgrad(int32_t n_groups, int32_t rows, int32_t N, int32_t K, const void* dC, int64_t lddc,
+                                        const void* A, int64_t lda, const int32_t* offsets, int32_t out_dtype,
+                                        int32_t accumulate, void* dB, void* workspace, size_t ws_bytes,
+                                        ec2moe_stream_t stream) {
+  reset_launch_count();
+  ec2moe_status st = check_grouped(n_groups, rows, N, K);
+  if (st != EC2MOE_OK) return st;
+  if (!known_dtype(out_dtype) || lddc < N || lda < K || (!offsets && n_groups != 1)) return EC2MOE_ERR_INVALID_ARG;
+  if (accumulate != 0 && (accumulate != 1 || out_dtype != EC2MOE_F32)) return EC2MOE_ERR_INVALID_ARG;
+  if (lddc % 8 != 0 || lda % 8 != 0) return EC2MOE_ERR_MISALIGNED;
+  EC2MOE_REQUIRE_PTR(dB);
+  if (rows == 0) {
+    const size_t bytes = static_cast<size_t>(n_groups) * N * K * (out_dtype == EC2MOE_BF16 ? 2 : 4);
+    if (!accumulate) EC2MOE_CUDA(cudaMemsetAsync(dB, 0, bytes, stream));
+    return EC2MOE_OK;
+  }
+  EC2MOE_REQUIRE_PTR(dC);
+  EC2MOE_REQUIRE_PTR(A);
+  GroupedArgs g{dC, lddc, A, lda, offsets, nullptr, n_groups, rows, N, K, dB, K};
+  g.accumulate = accumulate;
+  g.name = "grouped_wgrad";
+  return run_grouped(g, GROUPED_WGRAD, out_dtype, workspace, ws_bytes, stream);
+}
+
 ec2moe_status ec2moe_last_device_error(ec2moe_stream_t stream) {
   if (cudaStreamSynchronize(stream) != cudaSuccess) return EC2MOE_ERR_CUDA;
   unsigned int tc = 0, codec = 0, gate = 0, route = 0, swap = 0, skinny = 0, f32 = 0, tok = 0, fp8 = 0, fp8_swap = 0,
-               quant = 0, balance = 0, logits = 0;
+               quant = 0, balance = 0, logits = 0, act = 0, grouped = 0;
   if (read_tc_error(&tc) != cudaSuccess) return EC2MOE_ERR_CUDA;
   if (read_codec_error(&codec) != cudaSuccess) return EC2MOE_ERR_CUDA;
   if (read_gate_error(&gate) != cudaSuccess) return EC2MOE_ERR_CUDA;
@@ -1361,11 +1561,14 @@ ec2moe_status ec2moe_last_device_error(ec2moe_stream_t stream) {
   if (read_logits_error(&logits) != cudaSuccess) return EC2MOE_ERR_CUDA;
   if (read_quant_error(&quant) != cudaSuccess) return EC2MOE_ERR_CUDA;
   if (read_balance_error(&balance) != cudaSuccess) return EC2MOE_ERR_CUDA;
+  if (read_act_error(&act) != cudaSuccess) return EC2MOE_ERR_CUDA;
+  if (read_grouped_error(&grouped) != cudaSuccess) return EC2MOE_ERR_CUDA;
   // bit 0 of the GEMM, codec and gate words: a bounded wait timed out;
-  // bit 1 of the GEMM words and any bit of the routing, quantiser and balance
-  // words: an index outside the call's rows or experts was skipped
-  if ((tc | codec | gate | swap | f32 | tok | fp8 | logits) & 1u) return EC2MOE_ERR_TIMEOUT;
-  if (((tc | swap | skinny | f32 | tok | fp8) & 2u) || route || quant || balance) return EC2MOE_ERR_INVALID_ARG;
+  // bit 1 of the GEMM words and any bit of the routing, quantiser, balance and
+  // activation words: an index outside the call's rows or experts was skipped
+  if ((tc | codec | gate | swap | f32 | tok | fp8 | logits | grouped) & 1u) return EC2MOE_ERR_TIMEOUT;
+  if (((tc | swap | skinny | f32 | tok | fp8 | grouped) & 2u) || route || quant || balance || act)
+    return EC2MOE_ERR_INVALID_ARG;
   return EC2MOE_OK;
 }
 

@@ -362,6 +362,78 @@ cudaError_t launch_balance(const BalanceArgs& a, cudaStream_t s);
 // nonzero when an expert id or a segment bound out of range was skipped.
 cudaError_t read_balance_error(unsigned int* word);
 
+// ------------------------------------------- norm, activation, grouped products
+struct NormArgs {
+  const void* X;          // [rows, cols], pitch ld
+  const void* residual;   // the same, or nullptr
+  const float* weight;    // [cols], nullptr: ones
+  long long ld;
+  int rows, cols;
+  float eps;
+  void* H;                // X + residual, dense, or nullptr
+  float* rstd;            // [rows] or nullptr
+  void* Y;                // dense, or nullptr
+  void* Q;                // e4m3, dense, or nullptr; with it:
+  float* scale;           // [rows, ceil(cols / 128)]
+};
+struct NormBackArgs {
+  const void* dY;         // [rows, cols], pitch ld
+  const void* H;
+  const float* rstd;
+  const float* weight;    // nullptr: ones
+  const void* dH;         // nullptr: none
+  long long ld;
+  int rows, cols;
+  void* dX;
+  float* d_weight;        // nullptr: not wanted
+  float* partial;         // norm_backward_bytes(), when d_weight is wanted
+};
+constexpr int NORM_MAX_COLS = 16384;  // 512 threads of 4 x 8 columns
+size_t norm_backward_bytes(int rows, int cols);
+cudaError_t launch_rmsnorm(const NormArgs& a, bool bf16, bool y_bf16, cudaStream_t s);
+cudaError_t launch_rmsnorm_backward(const NormBackArgs& a, bool bf16, bool y_bf16, cudaStream_t s);
+
+struct ActArgs {
+  const void* U;          // [rows, cols], pitch ld, as V, dU, dV
+  const void* V;          // SwiGLU
+  long long ld;
+  int rows, cols;
+  const int32_t* perm;    // row -> slot, nullptr: itself
+  const float* row_scale; // by slot, nullptr: 1
+  const void* dH;         // gradient: [rows, cols] dense
+  void* dU;
+  void* dV;
+  void* H;                // [rows, cols] dense; gradient: nullptr: not wanted
+  float* d_row_scale;     // gradient: by slot, nullptr: not wanted
+};
+cudaError_t launch_activation(const ActArgs& a, bool bf16, bool glu, bool back, cudaStream_t s);
+// Reads and clears the activation's device error word (synchronous): nonzero when
+// a slot outside the call's rows was skipped.
+cudaError_t read_act_error(unsigned int* word);
+
+// Grouped bf16 products, group g owning rows [offsets[g], offsets[g + 1]):
+//   GROUPED_FWD    out_g = X_g W_g^T    X [rows, K], W [G, N, K], out [rows, N]
+//   GROUPED_DGRAD  out_g = X_g W_g      X [rows, N], W [G, N, K], out [rows, K]
+//   GROUPED_WGRAD  out_g = X_g^T W_g    X [rows, N], W [rows, K], out [G, N, K]
+enum GroupedForm { GROUPED_FWD = 0, GROUPED_DGRAD = 1, GROUPED_WGRAD = 2 };
+struct GroupedArgs {
+  const void* X; long long ldx;
+  const void* W; long long ldw;  // ldw: GROUPED_WGRAD
+  const int32_t* offsets;        // nullptr: one group of all rows
+  const int32_t* perm;           // destination of each row (FWD, DGRAD), nullptr: itself
+  int G, rows, N, K;
+  void* out; long long ldo;
+  bool out_bf16;
+  int accumulate;                // GROUPED_WGRAD, fp32: add to out
+  void* workspace;               // grouped_bytes()
+  long long timeout_cycles;
+  const char* name;
+};
+constexpr int GROUPED_MAX_SPLIT = 16;  // ranges of a split sum
+size_t grouped_bytes(int form, int G, int rows, int N, int K);
+cudaError_t launch_grouped(const GroupedArgs& a, int form, cudaStream_t s);
+cudaError_t read_grouped_error(unsigned int* word);  // bits as read_tc_error
+
 // Fused low-rank codec of the layer path (bf16): Z = X V_enc^T (stored), then
 // X_hat = Z V_dec^T written straight into expert order with relative
 // placement (see EPI_REPLICATE's relative mode), plus the tail rows

@@ -45,6 +45,9 @@ EXPORTED = [
     "ec2moe_fp8_quantize", "ec2moe_fp8_gemm_workspace_size", "ec2moe_fp8_gemm", "ec2moe_experts_fp8_workspace_size",
     "ec2moe_experts_fp8", "ec2moe_gate_logits_workspace_size", "ec2moe_gate_logits",
     "ec2moe_balance_loss_workspace_size", "ec2moe_balance_loss",
+    "ec2moe_rmsnorm", "ec2moe_rmsnorm_backward_workspace_size", "ec2moe_rmsnorm_backward", "ec2moe_activation",
+    "ec2moe_activation_backward", "ec2moe_grouped_gemm_workspace_size", "ec2moe_grouped_gemm",
+    "ec2moe_grouped_gemm_dgrad", "ec2moe_grouped_gemm_wgrad",
 ]
 
 FP8_BLOCK = 128  # columns (and weight rows) that share a scale
@@ -78,6 +81,9 @@ class Ec2moeError(RuntimeError):
 _lib: Optional[ctypes.CDLL] = None
 
 _P = ctypes.c_void_p
+_I = ctypes.c_int32
+_L = ctypes.c_int64
+_Z = ctypes.c_size_t
 _D = ctypes.POINTER(LayerDesc)
 _SIGS = {
     "ec2moe_workspace_size": (ctypes.c_size_t, [_D]),
@@ -125,6 +131,15 @@ _SIGS = {
     "ec2moe_balance_loss_workspace_size": (ctypes.c_size_t, [_D, ctypes.c_int32]),
     "ec2moe_balance_loss": (ctypes.c_int, [_D, _P, ctypes.c_int64, _P, _P, _P, _P, ctypes.c_int32, ctypes.c_float, _P,
                                            _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
+    "ec2moe_rmsnorm": (ctypes.c_int, [_I, _I, _I, _I, _L, _P, _P, _P, ctypes.c_float, _P, _P, _P, _P, _P, _P]),
+    "ec2moe_rmsnorm_backward_workspace_size": (_Z, [_I, _I]),
+    "ec2moe_rmsnorm_backward": (ctypes.c_int, [_I, _I, _I, _I, _L, _P, _P, _P, _P, _P, _P, _P, _P, _Z, _P]),
+    "ec2moe_activation": (ctypes.c_int, [_I, _I, _I, _I, _L, _P, _P, _P, _P, _P, _P]),
+    "ec2moe_activation_backward": (ctypes.c_int, [_I, _I, _I, _I, _L, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "ec2moe_grouped_gemm_workspace_size": (_Z, [_I, _I, _I, _I]),
+    "ec2moe_grouped_gemm": (ctypes.c_int, [_I, _I, _I, _I, _P, _L, _P, _P, _P, _I, _P, _L, _P, _Z, _P]),
+    "ec2moe_grouped_gemm_dgrad": (ctypes.c_int, [_I, _I, _I, _I, _P, _L, _P, _P, _P, _I, _P, _L, _P, _Z, _P]),
+    "ec2moe_grouped_gemm_wgrad": (ctypes.c_int, [_I, _I, _I, _I, _P, _L, _P, _L, _P, _I, _I, _P, _P, _Z, _P]),
 }
 
 
@@ -386,6 +401,69 @@ def ec2moe_balance_loss(desc, logits, ld, mask, topk_idx, valid, seg_offsets, n_
                                       _ptr(seg_offsets), int(n_seg), float(coef), _ptr(d_loss), _ptr(loss),
                                       _ptr(counts), _ptr(d_logits), _ptr(d_bias), _ptr(workspace), int(ws_bytes),
                                       _stream(stream)), "ec2moe_balance_loss")
+
+
+# ----------------------------------------------------------------- norm, activation, grouped products
+def ec2moe_rmsnorm(dtype, y_dtype, rows, cols, ld, X, residual, weight, eps, H=None, rstd=None, Y=None, Q=None,
+                   scale=None, stream=None):
+    """H = X + residual, Y = its root-mean-square norm times weight; Q, scale: Y in 8 bits."""
+    _check(load().ec2moe_rmsnorm(int(dtype), int(y_dtype), int(rows), int(cols), int(ld), _ptr(X), _ptr(residual),
+                                 _ptr(weight), float(eps), _ptr(H), _ptr(rstd), _ptr(Y), _ptr(Q), _ptr(scale),
+                                 _stream(stream)), "ec2moe_rmsnorm")
+
+
+def ec2moe_rmsnorm_backward_workspace_size(rows: int, cols: int) -> int:
+    return int(load().ec2moe_rmsnorm_backward_workspace_size(int(rows), int(cols)))
+
+
+def ec2moe_rmsnorm_backward(dtype, y_dtype, rows, cols, ld, dY, H, rstd, weight, dH, dX, d_weight=None, workspace=None,
+                            ws_bytes=0, stream=None):
+    """dX (of X and the residual) and d_weight from dY and the gradient dH that arrives at H."""
+    _check(load().ec2moe_rmsnorm_backward(int(dtype), int(y_dtype), int(rows), int(cols), int(ld), _ptr(dY), _ptr(H),
+                                          _ptr(rstd), _ptr(weight), _ptr(dH), _ptr(dX), _ptr(d_weight), _ptr(workspace),
+                                          int(ws_bytes), _stream(stream)), "ec2moe_rmsnorm_backward")
+
+
+def ec2moe_activation(dtype, act, rows, cols, ld, U, V, perm, row_scale, H, stream=None):
+    """H[p] = row_scale[perm[p]] * SiLU(U[p]) * V[p] (or GELU(U[p]))."""
+    _check(load().ec2moe_activation(int(dtype), int(act), int(rows), int(cols), int(ld), _ptr(U), _ptr(V), _ptr(perm),
+                                    _ptr(row_scale), _ptr(H), _stream(stream)), "ec2moe_activation")
+
+
+def ec2moe_activation_backward(dtype, act, rows, cols, ld, U, V, perm, row_scale, dH, dU, dV, H=None, d_row_scale=None,
+                               stream=None):
+    """dU, dV and d_row_scale from dH; H: the forward's again."""
+    _check(load().ec2moe_activation_backward(int(dtype), int(act), int(rows), int(cols), int(ld), _ptr(U), _ptr(V),
+                                             _ptr(perm), _ptr(row_scale), _ptr(dH), _ptr(dU), _ptr(dV), _ptr(H),
+                                             _ptr(d_row_scale), _stream(stream)), "ec2moe_activation_backward")
+
+
+def ec2moe_grouped_gemm_workspace_size(n_groups: int, rows: int, N: int, K: int) -> int:
+    return int(load().ec2moe_grouped_gemm_workspace_size(int(n_groups), int(rows), int(N), int(K)))
+
+
+def ec2moe_grouped_gemm(n_groups, rows, N, K, A, lda, offsets, B, perm, out_dtype, out, ldc, workspace=None, ws_bytes=0,
+                        stream=None):
+    """out_g = A_g B_g^T over the groups of rows that `offsets` names (None: one group), row p to row perm[p]."""
+    _check(load().ec2moe_grouped_gemm(int(n_groups), int(rows), int(N), int(K), _ptr(A), int(lda), _ptr(offsets), _ptr(B),
+                                      _ptr(perm), int(out_dtype), _ptr(out), int(ldc), _ptr(workspace), int(ws_bytes),
+                                      _stream(stream)), "ec2moe_grouped_gemm")
+
+
+def ec2moe_grouped_gemm_dgrad(n_groups, rows, N, K, dC, lddc, offsets, B, perm, out_dtype, dA, ldda, workspace=None,
+                              ws_bytes=0, stream=None):
+    """dA_g = dC_g B_g, row p to row perm[p]."""
+    _check(load().ec2moe_grouped_gemm_dgrad(int(n_groups), int(rows), int(N), int(K), _ptr(dC), int(lddc), _ptr(offsets),
+                                            _ptr(B), _ptr(perm), int(out_dtype), _ptr(dA), int(ldda), _ptr(workspace),
+                                            int(ws_bytes), _stream(stream)), "ec2moe_grouped_gemm_dgrad")
+
+
+def ec2moe_grouped_gemm_wgrad(n_groups, rows, N, K, dC, lddc, A, lda, offsets, out_dtype, accumulate, dB, workspace=None,
+                              ws_bytes=0, stream=None):
+    """dB_g = dC_g^T A_g, or (accumulate) added to it."""
+    _check(load().ec2moe_grouped_gemm_wgrad(int(n_groups), int(rows), int(N), int(K), _ptr(dC), int(lddc), _ptr(A),
+                                            int(lda), _ptr(offsets), int(out_dtype), int(accumulate), _ptr(dB),
+                                            _ptr(workspace), int(ws_bytes), _stream(stream)), "ec2moe_grouped_gemm_wgrad")
 
 
 # ----------------------------------------------------------------- scheduler (host)
