@@ -32,7 +32,7 @@
 // warp 2 reports to the even one's (tpeer), which arrives for both.
 //
 // Sums: the tensor core adds into its fp32 accumulator without rounding to
-// nearest, so sums are kept short: after `seg` blocks of 64 (4 for fp32 results, 128
+// nearest, so sums are kept short: after `seg` blocks of 64 (8 for fp32 results, 128
 // for bf16 ones) the accumulator is handed over and added to fp32 registers of
 // the epilogue, while the next segment fills the other one.
 //
@@ -48,6 +48,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <cmath>
 #include <mutex>
 #include <type_traits>
 
@@ -72,7 +73,7 @@ constexpr int BK = 64;   // sum elements per stage
 constexpr int UK = 16;   // sum elements of one tcgen05.mma kind::f16
 constexpr int CHUNK = 64 * BK * 2;  // bytes of an MN-major chunk: 64 sum rows of 128 bytes
 constexpr int EPI_WARPS = 16;
-constexpr int MAX_GROUPS = 136;
+constexpr int MAX_GROUPS = 128;
 constexpr int BOX = 16;  // rows of the small box that short tiles' rows come in
 
 enum Form { FWD = 0, DGRAD = 1, WGRAD = 2 };
@@ -83,7 +84,6 @@ struct Params {
   int cols;                // of the result
   int out_rows;            // WGRAD: rows of a group's result
   int depth;               // FWD, DGRAD: length of the sums
-  int tile;                // rows of the result per tile, a multiple of 32, at most BN
   int tiles_c, tiles_r;    // tiles along the columns; WGRAD: along the rows
   int band;                // tiles along the rows that are walked together
   int split;               // ranges of the sum
@@ -98,20 +98,22 @@ struct Params {
 
 constexpr int A_BYTES = BM * BK * 2;      // M side per CTA and stage
 constexpr int B_BYTES = BN / 2 * BK * 2;  // N side, at most
-constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
 constexpr int STAGES = 7;
 constexpr int TMEM_COLS = 2 * BN;
 // full, empty, tland, tpeer [STAGES]; tfull, tempty [2]; drain
 constexpr int N_BARS = 4 * STAGES + 5;
-constexpr int OFF_BARS = STAGES * STAGE_BYTES;
+constexpr int OFF_BARS = STAGES * (A_BYTES + B_BYTES);
 constexpr int OFF_SLOT = OFF_BARS + N_BARS * 8;
 constexpr int OFF_PREFIX = OFF_SLOT + 24;
 constexpr int OFF_ROW0 = OFF_PREFIX + (MAX_GROUPS + 1) * 4;
 constexpr int OFF_CNT = OFF_ROW0 + MAX_GROUPS * 4;
 constexpr int SMEM = 1024 + OFF_CNT + MAX_GROUPS * 4;
 static_assert(STAGES <= 16 && OFF_BARS % 8 == 0 && SMEM <= 232448, "shared memory per CTA");
-__host__ __device__ constexpr int first_epi(int form) { return form == WGRAD ? 3 : 2; }
-__host__ __device__ constexpr int threads(int form) { return 32 * (first_epi(form) + EPI_WARPS); }
+constexpr int FIRST_EPI = 4;  // the first warpgroup loads, issues and zeroes
+constexpr int THREADS = 32 * (FIRST_EPI + EPI_WARPS);
+// Registers: 640 threads start with 96 each (61440); the epilogue takes what the first
+// warpgroup gives up (128 * 56 + 512 * 104 = 60416).
+constexpr int REGS_FEW = 56, REGS_EPI = 104;
 
 struct Tile {
   int g, c, r0, n;   // group, column tile, first row (of the group, or of dB_g), rows
@@ -149,8 +151,8 @@ __device__ __forceinline__ Tile decode(const Params& p, int unit, const int* pre
   const int wide = min(p.band, tiles_r - band * p.band);
   rem -= band * p.band * p.tiles_c;
   t.c = rem / wide;
-  t.r0 = (band * p.band + rem % wide) * p.tile;
-  t.n = min(p.tile, n_rows - t.r0);
+  t.r0 = (band * p.band + rem % wide) * BN;
+  t.n = min(BN, n_rows - t.r0);
   t.nn = (t.n + 31) & ~31;
   const int n_kb = (t.len + BK - 1) / BK;
   const int per_split = (n_kb + p.split - 1) / p.split;
@@ -201,11 +203,11 @@ __device__ __forceinline__ void scan_groups(const Params& p, int lane, const Sha
   constexpr int CHUNKS = (MAX_GROUPS + 31) / 32;
   scan_group_rows<CHUNKS, 1>(p.offsets, p.G, p.rows, lane, sh.row0, sh.cnt, sh.prefix, &g_grouped_error);
   __syncwarp();
-  warp_exclusive_scan<CHUNKS>(p.G, lane, [&](int g) { return (sh.cnt[g] + p.tile - 1) / p.tile; }, sh.prefix);
+  warp_exclusive_scan<CHUNKS>(p.G, lane, [&](int g) { return (sh.cnt[g] + BN - 1) / BN; }, sh.prefix);
 }
 
-template <int FORM, bool F32>
-__global__ void __launch_bounds__(threads(FORM), 1)
+template <int FORM, bool F32, bool PERM>
+__global__ void __launch_bounds__(THREADS, 1)
     grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                         const __grid_constant__ CUtensorMap tmBox, const Params p) {
   constexpr bool A_MN = FORM != FWD, B_MN = FORM == WGRAD;
@@ -275,188 +277,193 @@ __global__ void __launch_bounds__(threads(FORM), 1)
   const int n_units = (FORM == WGRAD ? p.G * p.tiles_r : sh.prefix[p.G]) * p.tiles_c * p.split;
   const long long budget = p.timeout;
 
-  if (warp == 0) {
-    // ---------------------------------------------------------------- producer
-    const bool issue = elect_one();
-    int stage = 0;
-    uint32_t phase = 0;
-    uint32_t issued = 0, issued_phase = 0;  // bit s: stage s holds a copy, the phase that it completes
-    uint32_t tailed = 0, tailed_phase = 0;  // the same for copies that complete on tland
-    uint32_t tail_phase = 0;                // tland's next phase
-    int cursor = 0;
-    bool ok = true;
-    for (int unit = unit_first; unit < n_units && ok; unit += unit_step) {
-      const Tile t = decode<FORM>(p, unit, sh.prefix, sh.cnt, cursor);
-      const int row0 = sh.row0[t.g];
-      const int c0 = t.c * 2 * BM + static_cast<int>(rank) * BM;  // this CTA's columns
-      const int half = t.nn / 2;                                  // and its half of the rows
-      const int r0 = t.r0 + static_cast<int>(rank) * half;
-      const int b_bytes = B_MN ? (half + 63) / 64 * CHUNK : half * BK * 2;
-      for (int kb = t.kb0; kb < t.kb1; ++kb) {
-        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.empty[stage]), phase ^ 1u, budget, sh.abort_flag, &g_grouped_error))) {
-          ok = false;
-          break;
-        }
-        const int k0 = kb * BK;
-        const bool tail = FORM == WGRAD && t.len - k0 < BK && t.len % UK != 0;
-        if (issue) {
-          const uint32_t da = smem_u32(sh.sA + stage * A_BYTES), db = smem_u32(sh.sB + stage * B_BYTES);
-          if (FORM == WGRAD && tail) {
-            const uint32_t bar = smem_u32(&sh.tland[stage]);
-            mbar_expect_tx(bar, A_BYTES + b_bytes);
-            for (int c = 0; c < BM / 64; ++c) tma_load_2d(da + c * CHUNK, &tmA, c0 + c * 64, row0 + k0, bar);
-            for (int c = 0; c * 64 < half; ++c) tma_load_2d(db + c * CHUNK, &tmB, r0 + c * 64, row0 + k0, bar);
-          } else {
-            uint32_t bar = smem_u32(&sh.full[stage]);
-            // both CTAs' copies complete on the even CTA's barrier
-            if (rank == 0) mbar_expect_tx(bar, 2 * (A_BYTES + b_bytes));
-            else bar = map_to_rank(bar, 0);
-            if (FORM == WGRAD) {
-#pragma unroll
-              for (int c = 0; c < BM / 64; ++c) tma_load_2d_to_pair_bar(da + c * CHUNK, &tmA, c0 + c * 64, row0 + k0, bar);
-              for (int c = 0; c * 64 < half; ++c) tma_load_2d_to_pair_bar(db + c * CHUNK, &tmB, r0 + c * 64, row0 + k0, bar);
-            } else {
-              if (FORM == FWD) {
-                load_3d_to_pair_bar(da, &tmA, k0, c0, t.g, bar);
-              } else {
-#pragma unroll
-                for (int c = 0; c < BM / 64; ++c) load_3d_to_pair_bar(da + c * CHUNK, &tmA, c0 + c * 64, k0, t.g, bar);
-              }
-              if (half == BN / 2) {
-                tma_load_2d_to_pair_bar(db, &tmB, k0, row0 + r0, bar);
-              } else {
-                for (int b = 0; b < half; b += BOX) tma_load_2d_to_pair_bar(db + b * (BK * 2), &tmBox, k0, row0 + r0 + b, bar);
-              }
-            }
-          }
-        }
-        const uint32_t bit = 1u << stage;
-        if (tail) {
-          issued &= ~bit;
-          tailed |= bit;
-          tailed_phase = (tailed_phase & ~bit) | (tail_phase & bit);
-          tail_phase ^= bit;
-        } else {
-          tailed &= ~bit;
-          issued |= bit;
-          issued_phase = (issued_phase & ~bit) | (phase << stage);
-        }
-        if (++stage == STAGES) {
-          stage = 0;
-          phase ^= 1u;
-        }
-      }
-    }
-    if (lane == 0) {
-      sh.in_flight[0] = issued | (issued_phase << 16);
-      sh.in_flight[1] = tailed | (tailed_phase << 16);
-    }
-  } else if (warp == 1) {
-    if (rank == 0) {
-      // -------------------------------------------------------------- MMA issuer
+  if (warp < FIRST_EPI) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_FEW));
+    if (warp == 0) {
+      // ---------------------------------------------------------------- producer
       const bool issue = elect_one();
-      constexpr uint32_t IDESC0 = idesc_bf16(2 * BM, 0) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u);
-      // the address field's step per 16 sum elements: 32 bytes of a row, or 16 rows
-      constexpr uint64_t STEP_A = A_MN ? 16 * 128 / 16 : 2, STEP_B = B_MN ? 16 * 128 / 16 : 2;
-      const uint64_t da0 = A_MN ? sdesc_mn(smem_u32(sh.sA)) : sdesc_sw128(smem_u32(sh.sA));
-      const uint64_t db0 = B_MN ? sdesc_mn(smem_u32(sh.sB)) : sdesc_sw128(smem_u32(sh.sB));
       int stage = 0;
       uint32_t phase = 0;
-      uint32_t it = 0;  // segments so far: accumulator it & 1
+      uint32_t issued = 0, issued_phase = 0;  // bit s: stage s holds a copy, the phase that it completes
+      uint32_t tailed = 0, tailed_phase = 0;  // the same for copies that complete on tland
+      uint32_t tail_phase = 0;                // tland's next phase
       int cursor = 0;
-      bool ok = true, any = false;
+      bool ok = true;
       for (int unit = unit_first; unit < n_units && ok; unit += unit_step) {
         const Tile t = decode<FORM>(p, unit, sh.prefix, sh.cnt, cursor);
-        const uint32_t idesc = IDESC0 | (static_cast<uint32_t>(t.nn >> 3) << 17);
-        for (int s0 = t.kb0; s0 < t.kb1 && ok; s0 += p.seg, ++it) {
-          const uint32_t acc = it & 1u, acc_phase = (it >> 1) & 1u;
-          if (!__all_sync(0xffffffffu, mbar_wait_cluster(smem_u32(&sh.tempty[acc]), acc_phase ^ 1u, budget, sh.abort_flag,
-                                                         &g_grouped_error))) {
+        const int row0 = sh.row0[t.g];
+        const int c0 = t.c * 2 * BM + static_cast<int>(rank) * BM;  // this CTA's columns
+        const int half = t.nn / 2;                                  // and its half of the rows
+        const int r0 = t.r0 + static_cast<int>(rank) * half;
+        const int b_bytes = B_MN ? (half + 63) / 64 * CHUNK : half * BK * 2;
+        for (int kb = t.kb0; kb < t.kb1; ++kb) {
+          if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.empty[stage]), phase ^ 1u, budget, sh.abort_flag, &g_grouped_error))) {
             ok = false;
             break;
           }
-          tc_fence_after();
-          const uint32_t d = tmem_base + acc * BN;
-          const int s1 = min(s0 + p.seg, t.kb1);
-          for (int kb = s0; kb < s1; ++kb) {
-            const uint32_t fb = smem_u32(&sh.full[stage]);
-            const bool there = FORM == WGRAD ? mbar_wait_cluster(fb, phase, budget, sh.abort_flag, &g_grouped_error)
-                                             : mbar_wait(fb, phase, budget, sh.abort_flag, &g_grouped_error);
-            if (!__all_sync(0xffffffffu, there)) {
+          const int k0 = kb * BK;
+          const bool tail = FORM == WGRAD && t.len - k0 < BK && t.len % UK != 0;
+          if (issue) {
+            const uint32_t da = smem_u32(sh.sA + stage * A_BYTES), db = smem_u32(sh.sB + stage * B_BYTES);
+            if (FORM == WGRAD && tail) {
+              const uint32_t bar = smem_u32(&sh.tland[stage]);
+              mbar_expect_tx(bar, A_BYTES + b_bytes);
+              for (int c = 0; c < BM / 64; ++c) tma_load_2d(da + c * CHUNK, &tmA, c0 + c * 64, row0 + k0, bar);
+              for (int c = 0; c * 64 < half; ++c) tma_load_2d(db + c * CHUNK, &tmB, r0 + c * 64, row0 + k0, bar);
+            } else {
+              uint32_t bar = smem_u32(&sh.full[stage]);
+              // both CTAs' copies complete on the even CTA's barrier
+              if (rank == 0) mbar_expect_tx(bar, 2 * (A_BYTES + b_bytes));
+              else bar = map_to_rank(bar, 0);
+              if (FORM == WGRAD) {
+#pragma unroll
+                for (int c = 0; c < BM / 64; ++c) tma_load_2d_to_pair_bar(da + c * CHUNK, &tmA, c0 + c * 64, row0 + k0, bar);
+                for (int c = 0; c * 64 < half; ++c) tma_load_2d_to_pair_bar(db + c * CHUNK, &tmB, r0 + c * 64, row0 + k0, bar);
+              } else {
+                if (FORM == FWD) {
+                  load_3d_to_pair_bar(da, &tmA, k0, c0, t.g, bar);
+                } else {
+#pragma unroll
+                  for (int c = 0; c < BM / 64; ++c) load_3d_to_pair_bar(da + c * CHUNK, &tmA, c0 + c * 64, k0, t.g, bar);
+                }
+                if (half == BN / 2) {
+                  tma_load_2d_to_pair_bar(db, &tmB, k0, row0 + r0, bar);
+                } else {
+                  for (int b = 0; b < half; b += BOX) tma_load_2d_to_pair_bar(db + b * (BK * 2), &tmBox, k0, row0 + r0 + b, bar);
+                }
+              }
+            }
+          }
+          const uint32_t bit = 1u << stage;
+          if (tail) {
+            issued &= ~bit;
+            tailed |= bit;
+            tailed_phase = (tailed_phase & ~bit) | (tail_phase & bit);
+            tail_phase ^= bit;
+          } else {
+            tailed &= ~bit;
+            issued |= bit;
+            issued_phase = (issued_phase & ~bit) | (phase << stage);
+          }
+          if (++stage == STAGES) {
+            stage = 0;
+            phase ^= 1u;
+          }
+        }
+      }
+      if (lane == 0) {
+        sh.in_flight[0] = issued | (issued_phase << 16);
+        sh.in_flight[1] = tailed | (tailed_phase << 16);
+      }
+    } else if (warp == 1) {
+      if (rank == 0) {
+        // -------------------------------------------------------------- MMA issuer
+        const bool issue = elect_one();
+        constexpr uint32_t IDESC0 = idesc_bf16(2 * BM, 0) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u);
+        // the address field's step per 16 sum elements: 32 bytes of a row, or 16 rows
+        constexpr uint64_t STEP_A = A_MN ? 16 * 128 / 16 : 2, STEP_B = B_MN ? 16 * 128 / 16 : 2;
+        const uint64_t da0 = A_MN ? sdesc_mn(smem_u32(sh.sA)) : sdesc_sw128(smem_u32(sh.sA));
+        const uint64_t db0 = B_MN ? sdesc_mn(smem_u32(sh.sB)) : sdesc_sw128(smem_u32(sh.sB));
+        int stage = 0;
+        uint32_t phase = 0;
+        uint32_t it = 0;  // segments so far: accumulator it & 1
+        int cursor = 0;
+        bool ok = true, any = false;
+        for (int unit = unit_first; unit < n_units && ok; unit += unit_step) {
+          const Tile t = decode<FORM>(p, unit, sh.prefix, sh.cnt, cursor);
+          const uint32_t idesc = IDESC0 | (static_cast<uint32_t>(t.nn >> 3) << 17);
+          for (int s0 = t.kb0; s0 < t.kb1 && ok; s0 += p.seg, ++it) {
+            const uint32_t acc = it & 1u, acc_phase = (it >> 1) & 1u;
+            if (!__all_sync(0xffffffffu, mbar_wait_cluster(smem_u32(&sh.tempty[acc]), acc_phase ^ 1u, budget, sh.abort_flag,
+                                                           &g_grouped_error))) {
               ok = false;
               break;
             }
             tc_fence_after();
-            const uint64_t da = da0 + static_cast<uint64_t>(stage) * (A_BYTES >> 4);
-            const uint64_t db = db0 + static_cast<uint64_t>(stage) * (B_BYTES >> 4);
-            const int left = t.len - kb * BK;
-            if (issue) {
-#pragma unroll
-              for (int kk = 0; kk < BK / UK; ++kk) {
-                if (FORM == WGRAD && kk * UK >= left) break;
-                umma_bf16_pair(d, da + kk * STEP_A, db + kk * STEP_B, idesc, kb != s0 || kk != 0 ? 1u : 0u);
+            const uint32_t d = tmem_base + acc * BN;
+            const int s1 = min(s0 + p.seg, t.kb1);
+            for (int kb = s0; kb < s1; ++kb) {
+              const uint32_t fb = smem_u32(&sh.full[stage]);
+              const bool there = FORM == WGRAD ? mbar_wait_cluster(fb, phase, budget, sh.abort_flag, &g_grouped_error)
+                                               : mbar_wait(fb, phase, budget, sh.abort_flag, &g_grouped_error);
+              if (!__all_sync(0xffffffffu, there)) {
+                ok = false;
+                break;
               }
-              umma_commit_pair_mc(smem_u32(&sh.empty[stage]));
-            }
-            any = true;
-            if (++stage == STAGES) {
-              stage = 0;
-              phase ^= 1u;
-            }
-          }
-          if (ok && issue) umma_commit_pair_mc(smem_u32(&sh.tfull[acc]));
-        }
-      }
-      if (any && issue) sh.in_flight[2] = lane + 1;
-    }
-  } else if (FORM == WGRAD && warp == 2) {
-    // ------------------------------------------------- rows behind a group's end
-    uint32_t blocks = 0;      // so far
-    uint32_t tail_phase = 0;  // bit s: phase of stage s's tland and tpeer
-    int cursor = 0;
-    bool ok = true;
-    for (int unit = unit_first; unit < n_units && ok; unit += unit_step) {
-      const Tile t = decode<FORM>(p, unit, sh.prefix, sh.cnt, cursor);
-      blocks += static_cast<uint32_t>(t.kb1 - t.kb0);
-      const int left = t.len - (t.kb1 - 1) * BK;
-      if (t.kb1 <= t.kb0 || left >= BK || left % UK == 0) continue;
-      const uint32_t stage = (blocks - 1) % STAGES, bit = 1u << stage;
-      const uint32_t ph = (tail_phase & bit) ? 1u : 0u;
-      tail_phase ^= bit;
-      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.tland[stage]), ph, budget, sh.abort_flag, &g_grouped_error))) {
-        ok = false;
-        break;
-      }
-      // rows [left, end) of every chunk: 8 lanes per 128-byte row (the swizzle
-      // permutes within a row)
-      const int end = (left + UK - 1) / UK * UK;
-      for (int r = left + (lane >> 3); r < end; r += 4) {
-        const int at = r * 128 + (lane & 7) * 16;
+              tc_fence_after();
+              const uint64_t da = da0 + static_cast<uint64_t>(stage) * (A_BYTES >> 4);
+              const uint64_t db = db0 + static_cast<uint64_t>(stage) * (B_BYTES >> 4);
+              const int left = t.len - kb * BK;
+              if (issue) {
 #pragma unroll
-        for (int c = 0; c < BM / 64; ++c) {
-          *reinterpret_cast<U4*>(sh.sA + stage * A_BYTES + c * CHUNK + at) = U4{0, 0, 0, 0};
-          *reinterpret_cast<U4*>(sh.sB + stage * B_BYTES + c * CHUNK + at) = U4{0, 0, 0, 0};
+                for (int kk = 0; kk < BK / UK; ++kk) {
+                  if (FORM == WGRAD && kk * UK >= left) break;
+                  umma_bf16_pair(d, da + kk * STEP_A, db + kk * STEP_B, idesc, kb != s0 || kk != 0 ? 1u : 0u);
+                }
+                umma_commit_pair_mc(smem_u32(&sh.empty[stage]));
+              }
+              any = true;
+              if (++stage == STAGES) {
+                stage = 0;
+                phase ^= 1u;
+              }
+            }
+            if (ok && issue) umma_commit_pair_mc(smem_u32(&sh.tfull[acc]));
+          }
+        }
+        if (any && issue) sh.in_flight[2] = lane + 1;
+      }
+    } else if (warp == 2) {
+      if (FORM == WGRAD) {
+        // ------------------------------------------------- rows behind a group's end
+        uint32_t blocks = 0;      // so far
+        uint32_t tail_phase = 0;  // bit s: phase of stage s's tland and tpeer
+        int cursor = 0;
+        bool ok = true;
+        for (int unit = unit_first; unit < n_units && ok; unit += unit_step) {
+          const Tile t = decode<FORM>(p, unit, sh.prefix, sh.cnt, cursor);
+          blocks += static_cast<uint32_t>(t.kb1 - t.kb0);
+          const int left = t.len - (t.kb1 - 1) * BK;
+          if (t.kb1 <= t.kb0 || left >= BK || left % UK == 0) continue;
+          const uint32_t stage = (blocks - 1) % STAGES, bit = 1u << stage;
+          const uint32_t ph = (tail_phase & bit) ? 1u : 0u;
+          tail_phase ^= bit;
+          if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.tland[stage]), ph, budget, sh.abort_flag, &g_grouped_error))) {
+            ok = false;
+            break;
+          }
+          // rows [left, end) of every chunk: 8 lanes per 128-byte row (the swizzle
+          // permutes within a row)
+          const int end = (left + UK - 1) / UK * UK;
+          for (int r = left + (lane >> 3); r < end; r += 4) {
+            const int at = r * 128 + (lane & 7) * 16;
+#pragma unroll
+            for (int c = 0; c < BM / 64; ++c) *reinterpret_cast<U4*>(sh.sA + stage * A_BYTES + c * CHUNK + at) = U4{0, 0, 0, 0};
+            for (int c = 0; c * 64 < t.nn / 2; ++c)
+              *reinterpret_cast<U4*>(sh.sB + stage * B_BYTES + c * CHUNK + at) = U4{0, 0, 0, 0};
+          }
+          asm volatile("fence.proxy.async;" ::: "memory");
+          __syncwarp();
+          if (rank != 0) {
+            if (lane == 0) arrive_cluster(map_to_rank(smem_u32(&sh.tpeer[stage]), 0));
+            continue;
+          }
+          if (!__all_sync(0xffffffffu,
+                          mbar_wait_cluster(smem_u32(&sh.tpeer[stage]), ph, budget, sh.abort_flag, &g_grouped_error))) {
+            ok = false;
+            break;
+          }
+          if (lane == 0) arrive_cluster(smem_u32(&sh.full[stage]));
         }
       }
-      asm volatile("fence.proxy.async;" ::: "memory");
-      __syncwarp();
-      if (rank != 0) {
-        if (lane == 0) arrive_cluster(map_to_rank(smem_u32(&sh.tpeer[stage]), 0));
-        continue;
-      }
-      if (!__all_sync(0xffffffffu,
-                      mbar_wait_cluster(smem_u32(&sh.tpeer[stage]), ph, budget, sh.abort_flag, &g_grouped_error))) {
-        ok = false;
-        break;
-      }
-      if (lane == 0) arrive_cluster(smem_u32(&sh.full[stage]));
     }
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_EPI));
     // ---------------------------------------------------------------- epilogue
     // A thread's result column is its TMEM lane; its rows are the blocks of 16
     // part, part + 4, part + 8, part + 12.
     const int q = warp & 3;
-    const int part = (warp - first_epi(FORM)) >> 2;
+    const int part = (warp - FIRST_EPI) >> 2;
     constexpr int NB = BN / 64;  // blocks of a warp
     using OutT = typename std::conditional<F32, float, __nv_bfloat16>::type;
     uint32_t it = 0;
@@ -464,32 +471,28 @@ __global__ void __launch_bounds__(threads(FORM), 1)
     for (int unit = unit_first; unit < n_units; unit += unit_step) {
       const Tile t = decode<FORM>(p, unit, sh.prefix, sh.cnt, cursor);
       if (t.kb0 >= t.kb1 && (FORM != WGRAD || p.split > 1 || p.accumulate)) continue;  // nothing to add
-      // lane l: destinations of rows (l & 15) of the warp's blocks l / 16 and 2 + l / 16, -1: none
+      // With a perm, lane l: destinations of the rows l % 16 of the warp's blocks l / 16 and
+      // 2 + l / 16 (-1: none).  Without, the tile's rows follow each other.
       int dst[2];
+      const int first = FORM == WGRAD ? t.r0 : sh.row0[t.g] + t.r0;
+      if constexpr (PERM) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int r = (part + 4 * (2 * h + (lane >> 4))) * 16 + (lane & 15);
-        int d = -1;
-        if (r < t.n) {
-          d = FORM == WGRAD ? t.r0 + r : sh.row0[t.g] + t.r0 + r;
-          if (FORM != WGRAD && p.perm) {
-            d = p.perm[d];
-            if (d < 0 || d >= p.rows) {
-              atomicOr(&g_grouped_error, 2u);
-              d = -1;
-            }
+        for (int h = 0; h < 2; ++h) {
+          const int r = (part + 4 * (2 * h + (lane >> 4))) * 16 + (lane & 15);
+          dst[h] = r < t.n ? p.perm[first + r] : -1;
+          if (r < t.n && (dst[h] < 0 || dst[h] >= p.rows)) {
+            atomicOr(&g_grouped_error, 2u);
+            dst[h] = -1;
           }
         }
-        dst[h] = d;
       }
       float v[NB][16];
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[b][i] = 0.0f;
       bool ok = true;
-      if (t.kb0 >= t.kb1) {
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) v[b][i] = 0.0f;
-      }
+#pragma unroll 1
       for (int s0 = t.kb0; s0 < t.kb1; s0 += p.seg, ++it) {
         const uint32_t acc = it & 1u, acc_phase = (it >> 1) & 1u;
         if (!__all_sync(0xffffffffu,
@@ -499,24 +502,13 @@ __global__ void __launch_bounds__(threads(FORM), 1)
         }
         tc_fence_after();
         const uint32_t at = tmem_base + acc * BN + (static_cast<uint32_t>(q * 32) << 16) + part * 16;
-        if (s0 == t.kb0) {
-          uint32_t r[NB][16];
 #pragma unroll
-          for (int b = 0; b < NB; ++b) tmem_ld16_nw(at + b * 64, r[b]);
+        for (int b = 0; b < NB; ++b) {
+          uint32_t r[16];
+          tmem_ld16_nw(at + b * 64, r);
           tmem_wait();
 #pragma unroll
-          for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[b][i] = __uint_as_float(r[b][i]);
-        } else {
-#pragma unroll
-          for (int b = 0; b < NB; ++b) {
-            uint32_t r[16];
-            tmem_ld16_nw(at + b * 64, r);
-            tmem_wait();
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[b][i] += __uint_as_float(r[i]);
-          }
+          for (int i = 0; i < 16; ++i) v[b][i] += __uint_as_float(r[i]);
         }
         tc_fence_before();
         __syncwarp();
@@ -526,39 +518,57 @@ __global__ void __launch_bounds__(threads(FORM), 1)
       if (!ok) break;
       const int col = t.c * 2 * BM + static_cast<int>(rank) * BM + q * 32 + lane;
       const bool held = col < p.cols;
-      OutT* out = static_cast<OutT*>(p.out) + t.ks * p.part_stride;
+      const int odd = F32 ? 0 : lane & 1;
+      // where this lane's column (bf16: pair of columns) of row 0 lies
+      OutT* out = static_cast<OutT*>(p.out) + t.ks * p.part_stride + (col - odd);
       if (FORM == WGRAD) out += static_cast<long long>(t.g) * p.out_rows * p.ldo;
+      // bf16: two rows at a time, even lanes the first and the column beside theirs, odd
+      // lanes the second (the two halves of the lane's packed pair and its neighbour's)
+      const uint32_t pick = odd ? 0x3276u : 0x5410u;
+      if constexpr (PERM) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          if ((part + 4 * b) * 16 >= t.n) break;  // the whole warp
+#pragma unroll
+          for (int i = 0; i < 16; i += F32 ? 1 : 2) {
+            const int d = __shfl_sync(0xffffffffu, dst[b >> 1], (b & 1) * 16 + i + odd);
+            if constexpr (F32) {
+              if (d >= 0 && held) out[d * p.ldo] = v[b][i];
+            } else {
+              const uint32_t w = pack_bf16x2(v[b][i], v[b][i + 1]);
+              const uint32_t o = __byte_perm(w, __shfl_xor_sync(0xffffffffu, w, 1), pick);
+              if (d >= 0 && held) *reinterpret_cast<uint32_t*>(out + d * p.ldo) = o;
+            }
+          }
+        }
+        continue;
+      }
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         if ((part + 4 * b) * 16 >= t.n) break;  // the whole warp
+        OutT* to = out + (first + (part + 4 * b) * 16 + odd) * p.ldo;
+        const int n = held ? t.n - (part + 4 * b) * 16 - odd : 0;
         if constexpr (F32) {
-          // a row of the warp: 128 contiguous bytes
-          float o[16];
-          if (FORM == WGRAD && p.accumulate) {
+          // a row of the warp: 128 contiguous bytes; four rows at a time
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int d = __shfl_sync(0xffffffffu, dst[b >> 1], (b & 1) * 16 + i);
-              o[i] = d >= 0 && held ? out[d * p.ldo + col] : 0.0f;
+          for (int i = 0; i < 16; i += 4, to += 4 * p.ldo) {
+            if (FORM == WGRAD && p.accumulate) {
+              float o[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) o[j] = i + j < n ? to[j * p.ldo] : 0.0f;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) v[b][i + j] += o[j];
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[b][i] += o[i];
-          }
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int d = __shfl_sync(0xffffffffu, dst[b >> 1], (b & 1) * 16 + i);
-            if (d >= 0 && held) out[d * p.ldo + col] = v[b][i];
+            for (int j = 0; j < 4; ++j)
+              if (i + j < n) to[j * p.ldo] = v[b][i + j];
           }
         } else {
-          // two rows at a time: even lanes take the first and the column beside
-          // theirs, odd lanes the second, 64 contiguous bytes each
-          const int odd = lane & 1;
 #pragma unroll
-          for (int i = 0; i < 16; i += 2) {
-            const float give = odd ? v[b][i] : v[b][i + 1];
-            const float take = __shfl_xor_sync(0xffffffffu, give, 1);
-            const int d = __shfl_sync(0xffffffffu, dst[b >> 1], (b & 1) * 16 + i + odd);
-            const uint32_t w = odd ? pack_bf16x2(take, v[b][i + 1]) : pack_bf16x2(v[b][i], take);
-            if (d >= 0 && held) *reinterpret_cast<uint32_t*>(out + d * p.ldo + (col & ~1)) = w;
+          for (int i = 0; i < 16; i += 2, to += 2 * p.ldo) {
+            const uint32_t w = pack_bf16x2(v[b][i], v[b][i + 1]);
+            const uint32_t o = __byte_perm(w, __shfl_xor_sync(0xffffffffu, w, 1), pick);
+            if (i < n) *reinterpret_cast<uint32_t*>(to) = o;
           }
         }
       }
@@ -693,23 +703,51 @@ bool encode(CUtensorMap* m, const void* ptr, int mats, long long rows, long long
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// How a call is cut: rows of the result per tile, ranges of the sum.
-struct Plan {
-  int tile, split;
-};
-
-Plan plan_of(int form, int G, int rows, int N, int K) {
-  (void)form;
-  (void)G;
-  (void)rows;
-  (void)N;
-  (void)K;
-  return Plan{BN, 1};
+// Into how many ranges a call's sums are cut: the least of
+//   waves(tiles * S) * blocks of a range * 0.27 us, or what HBM needs if that is more,
+//   + for S > 1: 4.6 us and the partial results' way to the workspace and back
+// (0.27 us: a block of 64 of one tile at full clock; the others fitted to 700 x 512 x
+// 4096: one range 27 us, four 19, seven 17; 700 x 4096 x 4096: 27, two 41; the gradient
+// of 512 x 4096 weights over 8191 rows: 48, two 40, four 45; 32 rows of 8 experts of 4096
+// x 14336, bound by HBM: 139, two 160).  Ragged rows: the tiles are expected ones.
+int split_of(int form, int G, int rows, int N, int K) {
+  const int pairs = sm_count() / 2;
+  const int cols = form == FWD ? N : K;
+  const double tiles_c = (cols + 2 * BM - 1) / (2 * BM);
+  const int held = G < rows ? G : rows;  // groups with rows, at most
+  double tiles, out, bytes;
+  int n_kb;
+  if (form == WGRAD) {
+    tiles = tiles_c * G * ((N + BN - 1) / BN);
+    out = static_cast<double>(G) * N * K;
+    n_kb = (rows / G + BK - 1) / BK;
+    bytes = 2.0 * rows * (static_cast<double>(N) + K) + 2.0 * out;
+  } else {
+    tiles = tiles_c * (rows < held * BN ? held : rows / BN + 0.5 * held);
+    out = static_cast<double>(rows) * cols;
+    n_kb = ((form == FWD ? K : N) + BK - 1) / BK;
+    bytes = 2.0 * rows * (static_cast<double>(N) + K) + 2.0 * held * N * static_cast<double>(K);
+  }
+  const double hbm = bytes / 6.4e6;  // us
+  int best = 1;
+  double least = 0.0;
+  for (int s = 1; s <= GROUPED_MAX_SPLIT && (s == 1 || s * 4 <= n_kb); ++s) {
+    const int per = (n_kb + s - 1) / s;
+    if ((n_kb + per - 1) / per != s) continue;  // no empty range (FWD, DGRAD)
+    const double waves = ceil(tiles * s / pairs);
+    const double mma = waves * per * 0.27;
+    const double us = (mma > hbm ? mma : hbm) + (s > 1 ? 4.6 + s * out * 8.0 / 5e6 : 0.0);
+    if (s == 1 || us < least) {
+      best = s;
+      least = us;
+    }
+  }
+  return best;
 }
 
-template <int FORM, bool F32>
-cudaError_t launch(const GroupedArgs& a, const Plan& plan, cudaStream_t s) {
-  auto kernel = grouped_gemm_kernel<FORM, F32>;
+template <int FORM, bool F32, bool PERM>
+cudaError_t launch(const GroupedArgs& a, int split, cudaStream_t s) {
+  auto kernel = grouped_gemm_kernel<FORM, F32, PERM>;
   const void* kfn = reinterpret_cast<const void*>(kernel);
   cudaError_t e = ensure_smem_attr(kfn, SMEM);
   if (e != cudaSuccess) return e;
@@ -724,7 +762,7 @@ cudaError_t launch(const GroupedArgs& a, const Plan& plan, cudaStream_t s) {
            encode(&mB, a.X, 0, a.rows, depth, a.ldx, BN / 2) && encode(&mBox, a.X, 0, a.rows, depth, a.ldx, BOX);
   }
   if (!good) return cudaErrorInvalidValue;
-  const bool parts = plan.split > 1;
+  const bool parts = split > 1;
   Params p{};
   p.offsets = a.offsets;
   p.G = a.G;
@@ -732,26 +770,25 @@ cudaError_t launch(const GroupedArgs& a, const Plan& plan, cudaStream_t s) {
   p.cols = FORM == FWD ? a.N : a.K;
   p.out_rows = a.N;
   p.depth = FORM == FWD ? a.K : a.N;
-  p.tile = plan.tile;
   p.tiles_c = (p.cols + 2 * BM - 1) / (2 * BM);
-  p.tiles_r = (a.N + plan.tile - 1) / plan.tile;
+  p.tiles_r = (a.N + BN - 1) / BN;
   p.band = 8;
-  p.split = plan.split;
-  p.seg = F32 ? 4 : 128;
+  p.split = split;
+  p.seg = F32 ? 8 : 128;
   p.perm = parts ? nullptr : a.perm;
   p.out = parts ? a.workspace : a.out;
   p.ldo = parts ? p.cols : a.ldo;
   p.part_stride = parts ? (FORM == WGRAD ? static_cast<long long>(a.G) * a.N : a.rows) * static_cast<long long>(p.cols) : 0;
   p.accumulate = parts ? 0 : a.accumulate;
   p.timeout = a.timeout_cycles;
-  const long long row_tiles = FORM == WGRAD ? static_cast<long long>(a.G) * p.tiles_r : a.rows / plan.tile + a.G;
+  const long long row_tiles = FORM == WGRAD ? static_cast<long long>(a.G) * p.tiles_r : a.rows / BN + a.G;
   const long long units = row_tiles * p.tiles_c * p.split;
-  int clusters = max_clusters(kfn, threads(FORM), SMEM, 2);
+  int clusters = max_clusters(kfn, THREADS, SMEM, 2);
   if (clusters < 1) return cudaErrorInvalidConfiguration;
   if (units < clusters) clusters = static_cast<int>(units);
   {
     KernelScope ks(a.name, s);
-    e = launch_cluster(kernel, clusters, 2, threads(FORM), (size_t)SMEM, s, mA, mB, mBox, p);
+    e = launch_cluster(kernel, clusters, 2, THREADS, (size_t)SMEM, s, mA, mB, mBox, p);
     if (e != cudaSuccess) return e;
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
@@ -762,7 +799,7 @@ cudaError_t launch(const GroupedArgs& a, const Plan& plan, cudaStream_t s) {
   j.G = a.G;
   j.rows = a.rows;
   j.N = p.cols;
-  j.split = plan.split;
+  j.split = split;
   j.wgrad_rows = FORM == WGRAD ? a.N : 0;
   j.part = static_cast<const float*>(a.workspace);
   j.part_stride = p.part_stride;
@@ -782,18 +819,22 @@ cudaError_t launch(const GroupedArgs& a, const Plan& plan, cudaStream_t s) {
 
 template <int FORM>
 cudaError_t launch_form(const GroupedArgs& a, cudaStream_t s) {
-  const Plan plan = plan_of(FORM, a.G, a.rows, a.N, a.K);
-  return !a.out_bf16 || plan.split > 1 ? launch<FORM, true>(a, plan, s) : launch<FORM, false>(a, plan, s);
+  const int split = split_of(FORM, a.G, a.rows, a.N, a.K);
+  const bool f32 = !a.out_bf16 || split > 1;
+  if constexpr (FORM != WGRAD) {
+    if (a.perm && split == 1) return f32 ? launch<FORM, true, true>(a, 1, s) : launch<FORM, false, true>(a, 1, s);
+  }
+  return f32 ? launch<FORM, true, false>(a, split, s) : launch<FORM, false, false>(a, split, s);
 }
 
 }  // namespace
 
 size_t grouped_bytes(int form, int G, int rows, int N, int K) {
-  const Plan plan = plan_of(form, G, rows, N, K);
-  if (plan.split == 1) return 0;
+  const int split = split_of(form, G, rows, N, K);
+  if (split == 1) return 0;
   const size_t out = form == GROUPED_WGRAD ? static_cast<size_t>(G) * N * K
                                            : static_cast<size_t>(rows) * (form == GROUPED_FWD ? N : K);
-  return plan.split * out * 4;
+  return split * out * 4;
 }
 
 cudaError_t launch_grouped(const GroupedArgs& a, int form, cudaStream_t s) {

@@ -2,7 +2,7 @@
 
 Error of one element, with S the sum of its terms' magnitudes.  A tensor core's step
 adds 16 products to the fp32 accumulator; each of its 17 addends is cut below 2^-23 of the
-largest (at most S): 17 2^-23 S.  fp32 results hand a segment of 16 steps over: 272 2^-23 S at
+largest (at most S): 17 2^-23 S.  fp32 results hand a segment of 32 steps over: 544 2^-23 S at
 most over all segments together (each segment's bound is of its own S), and the segments'
 sums are added with 2^-24 S each.  bf16 results take segments of 512 steps, and are rounded by
 2^-8 of themselves.
@@ -26,7 +26,7 @@ def lib():
 
 
 def tolerance(value, mag, out, length):
-    per_segment, steps = (16, length // 16 + 1) if out == C.F32 else (512, length // 16 + 1)
+    per_segment, steps = (32, length // 16 + 1) if out == C.F32 else (512, length // 16 + 1)
     segments = steps // per_segment + 17  # and the ranges of a split sum, which has fp32 segments
     bound = (17 * min(per_segment, steps) * 2.0 ** -23 + segments * 2.0 ** -24) * mag
     return bound if out == C.F32 else bound + 2.0 ** -8 * value.abs()
