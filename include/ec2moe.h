@@ -499,9 +499,10 @@ ec2moe_status ec2moe_balance_loss(const ec2moe_layer_desc* desc, const float* lo
  *  H               out, dense, or NULL: h; may be X or residual itself where ld = cols
  *  rstd            out fp32 [rows], or NULL (ec2moe_rmsnorm_backward needs it)
  *  Y               out, dense, or NULL
- *  Q, scale        out, or both NULL: y as ec2moe_fp8_quantize stores rows (block_rows =
- *                  1), from the fp32 y: e4m3 [rows, cols], dense, and fp32 [rows,
- *                  ceil(cols / 128)]; what ec2moe_fp8_gemm and ec2moe_experts_fp8 take
+ *  Q, scale        out, or both NULL: y in 8 bits as ec2moe_fp8_quantize stores rows
+ *                  (block_rows = 1), rounded once, from y itself: e4m3 [rows, cols],
+ *                  dense, and fp32 [rows, ceil(cols / 128)]; what ec2moe_fp8_gemm and
+ *                  ec2moe_experts_fp8 take
  * One output at least.  cols is a multiple of 8 (with Q of 16), at most 16384 (more
  * return EC2MOE_ERR_UNSUPPORTED).  The squares are summed in fp32: where that sum
  * overflows y is 0, as it is for a row with an infinity, whose infinite elements become NaN;

@@ -1392,7 +1392,7 @@ ec2moe_status ec2moe_rmsnorm(int32_t dtype, int32_t y_dtype, int32_t rows, int32
   EC2MOE_REQUIRE_PTR(X);
   if (!aligned16(residual) || !aligned16(weight) || !aligned16(H) || !aligned16(Y) || !aligned16(Q))
     return EC2MOE_ERR_MISALIGNED;
-  const NormArgs a{X, residual, weight, ld, rows, cols, eps, H, rstd, Y, Q, scale};
+  const NormArgs a{X, residual, weight, ld, rows, cols, eps, H, rstd, Y, Q, scale, default_timeout_cycles()};
   EC2MOE_CUDA(launch_rmsnorm(a, dtype == EC2MOE_BF16, y_dtype == EC2MOE_BF16, stream));
   return EC2MOE_OK;
 }
@@ -1423,7 +1423,8 @@ ec2moe_status ec2moe_rmsnorm_backward(int32_t dtype, int32_t y_dtype, int32_t ro
   if (!rstd) return EC2MOE_ERR_INVALID_ARG;
   if (d_weight && (!workspace || ws_bytes < ec2moe_rmsnorm_backward_workspace_size(rows, cols))) return EC2MOE_ERR_WORKSPACE;
   if (d_weight && !aligned16(workspace)) return EC2MOE_ERR_MISALIGNED;
-  const NormBackArgs a{dY, H, rstd, weight, dH, ld, rows, cols, dX, d_weight, static_cast<float*>(workspace)};
+  const NormBackArgs a{dY, H, rstd, weight, dH, ld, rows, cols, dX, d_weight, static_cast<float*>(workspace),
+                       default_timeout_cycles()};
   EC2MOE_CUDA(launch_rmsnorm_backward(a, dtype == EC2MOE_BF16, y_dtype == EC2MOE_BF16, stream));
   return EC2MOE_OK;
 }
@@ -1546,7 +1547,7 @@ ec2moe_status ec2moe_grouped_gemm_wgrad(int32_t n_groups, int32_t rows, int32_t 
 ec2moe_status ec2moe_last_device_error(ec2moe_stream_t stream) {
   if (cudaStreamSynchronize(stream) != cudaSuccess) return EC2MOE_ERR_CUDA;
   unsigned int tc = 0, codec = 0, gate = 0, route = 0, swap = 0, skinny = 0, f32 = 0, tok = 0, fp8 = 0, fp8_swap = 0,
-               quant = 0, balance = 0, logits = 0, act = 0, grouped = 0;
+               quant = 0, balance = 0, logits = 0, act = 0, grouped = 0, norm = 0;
   if (read_tc_error(&tc) != cudaSuccess) return EC2MOE_ERR_CUDA;
   if (read_codec_error(&codec) != cudaSuccess) return EC2MOE_ERR_CUDA;
   if (read_gate_error(&gate) != cudaSuccess) return EC2MOE_ERR_CUDA;
@@ -1561,12 +1562,13 @@ ec2moe_status ec2moe_last_device_error(ec2moe_stream_t stream) {
   if (read_logits_error(&logits) != cudaSuccess) return EC2MOE_ERR_CUDA;
   if (read_quant_error(&quant) != cudaSuccess) return EC2MOE_ERR_CUDA;
   if (read_balance_error(&balance) != cudaSuccess) return EC2MOE_ERR_CUDA;
+  if (read_norm_error(&norm) != cudaSuccess) return EC2MOE_ERR_CUDA;
   if (read_act_error(&act) != cudaSuccess) return EC2MOE_ERR_CUDA;
   if (read_grouped_error(&grouped) != cudaSuccess) return EC2MOE_ERR_CUDA;
   // bit 0 of the GEMM, codec and gate words: a bounded wait timed out;
   // bit 1 of the GEMM words and any bit of the routing, quantiser, balance and
   // activation words: an index outside the call's rows or experts was skipped
-  if ((tc | codec | gate | swap | f32 | tok | fp8 | logits | grouped) & 1u) return EC2MOE_ERR_TIMEOUT;
+  if ((tc | codec | gate | swap | f32 | tok | fp8 | logits | grouped | norm) & 1u) return EC2MOE_ERR_TIMEOUT;
   if (((tc | swap | skinny | f32 | tok | fp8 | grouped) & 2u) || route || quant || balance || act)
     return EC2MOE_ERR_INVALID_ARG;
   return EC2MOE_OK;

