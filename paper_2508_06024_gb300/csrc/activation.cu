@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(THREADS) activation_kernel(const ActArgs a, in
 }
 
 template <typename T, bool GLU>
-__global__ void __launch_bounds__(THREADS) activation_backward_kernel(const ActArgs a, int tpr) {
+__global__ void __launch_bounds__(THREADS, 3) activation_backward_kernel(const ActArgs a, int tpr) {
   pdl_trigger();
   pdl_wait();
   __shared__ float s_sum[THREADS / 32];
@@ -80,7 +80,7 @@ __global__ void __launch_bounds__(THREADS) activation_backward_kernel(const ActA
     T* du = static_cast<T*>(a.dU) + row * a.ld;
     T* dv = static_cast<T*>(a.dV) + row * a.ld;
     T* h = static_cast<T*>(a.H) + row * a.cols;
-#pragma unroll 1
+#pragma unroll 2
     for (int c = t * PER; c < a.cols; c += tpr * PER) {
       float x[PER], y[PER], g[PER], o[PER];
       load8(u + c, x);

@@ -423,26 +423,26 @@ __global__ void __launch_bounds__(RING_THREADS, 1) rmsnorm_backward_kernel(const
   }
 }
 
-// out[c] = sum of partial[0 .. n)[c]: 32 columns per CTA, its warps take every
-// eighth row, their sums are added in order.
-__global__ void __launch_bounds__(256) dweight_sum_kernel(const float* partial, int n, int cols, float* out) {
+// out[c] = sum of partial[0 .. n)[c]: 32 columns per CTA, its warps take every 32nd row
+// (so that the few rows are fetched at once), their sums are added in order.
+__global__ void __launch_bounds__(1024) dweight_sum_kernel(const float* partial, int n, int cols, float* out) {
   pdl_trigger();
   pdl_wait();
-  __shared__ float s[8][32];
+  __shared__ float s[32][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int c = blockIdx.x * 32 + lane;
   float v = 0.0f;
   if (c < cols) {
 #pragma unroll 8
-    for (int r = warp; r < n; r += 8) v += partial[static_cast<long long>(r) * cols + c];
+    for (int r = warp; r < n; r += 32) v += partial[static_cast<long long>(r) * cols + c];
   }
   s[warp][lane] = v;
   __syncthreads();
-  if (warp == 0 && c < cols) {
+  // warp w adds up column w
+  v = s[lane][warp];
 #pragma unroll
-    for (int w = 1; w < 8; ++w) v += s[w][lane];
-    out[c] = v;
-  }
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if (lane == 0 && blockIdx.x * 32 + warp < cols) out[blockIdx.x * 32 + warp] = v;
 }
 
 template <typename TX, typename TY>
@@ -480,7 +480,7 @@ cudaError_t backward(const NormBackArgs& a, cudaStream_t s) {
   }
   if (!a.d_weight) return cudaSuccess;
   KernelScope ks("rmsnorm_dweight", s);
-  e = launch_kernel(dweight_sum_kernel, dim3((a.cols + 31) / 32), dim3(256), 0, s, a.partial, g.grid, a.cols, a.d_weight);
+  e = launch_kernel(dweight_sum_kernel, dim3((a.cols + 31) / 32), dim3(1024), 0, s, a.partial, g.grid, a.cols, a.d_weight);
   if (e != cudaSuccess) return e;
   return cudaGetLastError();
 }
