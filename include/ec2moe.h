@@ -292,8 +292,8 @@ ec2moe_status ec2moe_last_device_error(ec2moe_stream_t stream);
  * return; ec2moe_last_device_error then reports EC2MOE_ERR_TIMEOUT and the
  * context stays usable.  With a budget of 0 a wait gives up when the hardware's
  * own try (which may suspend for a few microseconds) finds it unsatisfied, and
- * the fp32 GEMM's waits for its accumulators and those of the 8-bit products and
- * the gate logits for their operands at once; that is how failure handling is
+ * the fp32 GEMM's and the grouped products' waits for their accumulators, those of
+ * the 8-bit products and the gate logits for their operands and the norm's for its rows at once; that is how failure handling is
  * exercised without a real fault.  Negative values return
  * EC2MOE_ERR_INVALID_ARG. */
 ec2moe_status ec2moe_set_wait_budget(int64_t cycles);
@@ -523,13 +523,13 @@ size_t ec2moe_rmsnorm_backward_workspace_size(int32_t rows, int32_t cols);
  *            stream behind the norm)
  *  dX        out, dtype, dense: the gradient of X and of residual; may be dH, H or (of
  *            the same type, ld = cols) dY itself
- *  d_weight  out fp32 [cols], or NULL (no workspace then)
+ *  d_weight  out fp32 [cols], or NULL (no workspace then); accumulate 1: it is added to
  * The sums are in a fixed order: the same inputs give the same bits.  No rows: d_weight
- * is 0. */
+ * is 0 (accumulate: as it was). */
 ec2moe_status ec2moe_rmsnorm_backward(int32_t dtype, int32_t y_dtype, int32_t rows, int32_t cols, int64_t ld,
                                       const void* dY, const void* H, const float* rstd, const float* weight,
-                                      const void* dH, void* dX, float* d_weight, void* workspace, size_t ws_bytes,
-                                      ec2moe_stream_t stream);
+                                      const void* dH, void* dX, float* d_weight, int32_t accumulate, void* workspace,
+                                      size_t ws_bytes, ec2moe_stream_t stream);
 
 /* The experts' activation of rows in expert order, with each row's gate weight:
  *   H[p] = row_scale[perm[p]] * a[p],  a = SiLU(U) * V  or  GELU(U)  (exact erf form)

@@ -1404,17 +1404,18 @@ size_t ec2moe_rmsnorm_backward_workspace_size(int32_t rows, int32_t cols) {
 
 ec2moe_status ec2moe_rmsnorm_backward(int32_t dtype, int32_t y_dtype, int32_t rows, int32_t cols, int64_t ld,
                                       const void* dY, const void* H, const float* rstd, const float* weight,
-                                      const void* dH, void* dX, float* d_weight, void* workspace, size_t ws_bytes,
-                                      ec2moe_stream_t stream) {
+                                      const void* dH, void* dX, float* d_weight, int32_t accumulate, void* workspace,
+                                      size_t ws_bytes, ec2moe_stream_t stream) {
   reset_launch_count();
   ec2moe_status st = check_rows(dtype, rows, cols, cols);
   if (st != EC2MOE_OK) return st;
+  if (accumulate != 0 && accumulate != 1) return EC2MOE_ERR_INVALID_ARG;
   st = check_rows(y_dtype, rows, cols, ld);
   if (st != EC2MOE_OK) return st;
   if (cols > NORM_MAX_COLS) return EC2MOE_ERR_UNSUPPORTED;
   if (!aligned16(weight) || !aligned16(dH) || !aligned16(d_weight)) return EC2MOE_ERR_MISALIGNED;
   if (rows == 0) {
-    if (d_weight) EC2MOE_CUDA(cudaMemsetAsync(d_weight, 0, static_cast<size_t>(cols) * 4, stream));
+    if (d_weight && !accumulate) EC2MOE_CUDA(cudaMemsetAsync(d_weight, 0, static_cast<size_t>(cols) * 4, stream));
     return EC2MOE_OK;
   }
   EC2MOE_REQUIRE_PTR(dY);
@@ -1423,8 +1424,8 @@ ec2moe_status ec2moe_rmsnorm_backward(int32_t dtype, int32_t y_dtype, int32_t ro
   if (!rstd) return EC2MOE_ERR_INVALID_ARG;
   if (d_weight && (!workspace || ws_bytes < ec2moe_rmsnorm_backward_workspace_size(rows, cols))) return EC2MOE_ERR_WORKSPACE;
   if (d_weight && !aligned16(workspace)) return EC2MOE_ERR_MISALIGNED;
-  const NormBackArgs a{dY, H, rstd, weight, dH, ld, rows, cols, dX, d_weight, static_cast<float*>(workspace),
-                       default_timeout_cycles()};
+  const NormBackArgs a{dY, H, rstd, weight, dH, ld, rows, cols, dX, d_weight, accumulate,
+                       static_cast<float*>(workspace), default_timeout_cycles()};
   EC2MOE_CUDA(launch_rmsnorm_backward(a, dtype == EC2MOE_BF16, y_dtype == EC2MOE_BF16, stream));
   return EC2MOE_OK;
 }

@@ -496,7 +496,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       for (int s0 = t.kb0; s0 < t.kb1; s0 += p.seg, ++it) {
         const uint32_t acc = it & 1u, acc_phase = (it >> 1) & 1u;
         if (!__all_sync(0xffffffffu,
-                        mbar_wait(smem_u32(&sh.tfull[acc]), acc_phase, budget, sh.abort_flag, &g_grouped_error))) {
+                        mbar_wait_strict(smem_u32(&sh.tfull[acc]), acc_phase, budget, sh.abort_flag, &g_grouped_error))) {
           ok = false;
           break;
         }

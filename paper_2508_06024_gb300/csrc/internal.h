@@ -387,6 +387,7 @@ struct NormBackArgs {
   int rows, cols;
   void* dX;
   float* d_weight;        // nullptr: not wanted
+  int accumulate;         // add to d_weight
   float* partial;         // norm_backward_bytes(), when d_weight is wanted
   long long timeout_cycles;
 };

@@ -271,7 +271,7 @@ __global__ void __launch_bounds__(RING_THREADS, 1) rmsnorm_ring_kernel(const Nor
   volatile int no_abort = 0;
   long long row = first;
   for (; row < a.rows; row += step) {
-    bool ok = mbar_wait(smem_u32(&full[team][d]), phase, a.timeout_cycles, &no_abort, &g_norm_error);
+    bool ok = mbar_wait_strict(smem_u32(&full[team][d]), phase, a.timeout_cycles, &no_abort, &g_norm_error);
     const TX* x = reinterpret_cast<const TX*>(mine_ring + d * g.bytes);
     const TX* res = x + a.cols;
     float h[NCH][PER];
@@ -354,7 +354,7 @@ __global__ void __launch_bounds__(RING_THREADS, 1) rmsnorm_backward_kernel(const
   long long row = first;
   for (; row < a.rows; row += step) {
     const float rstd = a.rstd[row];
-    bool ok = mbar_wait(smem_u32(&full[team][d]), phase, a.timeout_cycles, &no_abort, &g_norm_error);
+    bool ok = mbar_wait_strict(smem_u32(&full[team][d]), phase, a.timeout_cycles, &no_abort, &g_norm_error);
     const TY* dy = reinterpret_cast<const TY*>(mine_ring + d * g.bytes);
     const TX* h = reinterpret_cast<const TX*>(mine_ring + d * g.bytes + part_y);
     const TX* dh = h + a.cols;
@@ -425,7 +425,8 @@ __global__ void __launch_bounds__(RING_THREADS, 1) rmsnorm_backward_kernel(const
 
 // out[c] = sum of partial[0 .. n)[c]: 32 columns per CTA, its warps take every 32nd row
 // (so that the few rows are fetched at once), their sums are added in order.
-__global__ void __launch_bounds__(1024) dweight_sum_kernel(const float* partial, int n, int cols, float* out) {
+__global__ void __launch_bounds__(1024) dweight_sum_kernel(const float* partial, int n, int cols, float* out,
+                                                           int accumulate) {
   pdl_trigger();
   pdl_wait();
   __shared__ float s[32][33];
@@ -442,7 +443,10 @@ __global__ void __launch_bounds__(1024) dweight_sum_kernel(const float* partial,
   v = s[lane][warp];
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  if (lane == 0 && blockIdx.x * 32 + warp < cols) out[blockIdx.x * 32 + warp] = v;
+  if (lane == 0 && blockIdx.x * 32 + warp < cols) {
+    float* to = out + blockIdx.x * 32 + warp;
+    *to = accumulate ? *to + v : v;
+  }
 }
 
 template <typename TX, typename TY>
@@ -480,7 +484,8 @@ cudaError_t backward(const NormBackArgs& a, cudaStream_t s) {
   }
   if (!a.d_weight) return cudaSuccess;
   KernelScope ks("rmsnorm_dweight", s);
-  e = launch_kernel(dweight_sum_kernel, dim3((a.cols + 31) / 32), dim3(1024), 0, s, a.partial, g.grid, a.cols, a.d_weight);
+  e = launch_kernel(dweight_sum_kernel, dim3((a.cols + 31) / 32), dim3(1024), 0, s, a.partial, g.grid, a.cols, a.d_weight,
+                    a.accumulate);
   if (e != cudaSuccess) return e;
   return cudaGetLastError();
 }

@@ -133,7 +133,7 @@ _SIGS = {
                                            _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
     "ec2moe_rmsnorm": (ctypes.c_int, [_I, _I, _I, _I, _L, _P, _P, _P, ctypes.c_float, _P, _P, _P, _P, _P, _P]),
     "ec2moe_rmsnorm_backward_workspace_size": (_Z, [_I, _I]),
-    "ec2moe_rmsnorm_backward": (ctypes.c_int, [_I, _I, _I, _I, _L, _P, _P, _P, _P, _P, _P, _P, _P, _Z, _P]),
+    "ec2moe_rmsnorm_backward": (ctypes.c_int, [_I, _I, _I, _I, _L, _P, _P, _P, _P, _P, _P, _P, _I, _P, _Z, _P]),
     "ec2moe_activation": (ctypes.c_int, [_I, _I, _I, _I, _L, _P, _P, _P, _P, _P, _P]),
     "ec2moe_activation_backward": (ctypes.c_int, [_I, _I, _I, _I, _L, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P]),
     "ec2moe_grouped_gemm_workspace_size": (_Z, [_I, _I, _I, _I]),
@@ -417,11 +417,11 @@ def ec2moe_rmsnorm_backward_workspace_size(rows: int, cols: int) -> int:
 
 
 def ec2moe_rmsnorm_backward(dtype, y_dtype, rows, cols, ld, dY, H, rstd, weight, dH, dX, d_weight=None, workspace=None,
-                            ws_bytes=0, stream=None):
+                            ws_bytes=0, stream=None, accumulate=0):
     """dX (of X and the residual) and d_weight from dY and the gradient dH that arrives at H."""
     _check(load().ec2moe_rmsnorm_backward(int(dtype), int(y_dtype), int(rows), int(cols), int(ld), _ptr(dY), _ptr(H),
-                                          _ptr(rstd), _ptr(weight), _ptr(dH), _ptr(dX), _ptr(d_weight), _ptr(workspace),
-                                          int(ws_bytes), _stream(stream)), "ec2moe_rmsnorm_backward")
+                                          _ptr(rstd), _ptr(weight), _ptr(dH), _ptr(dX), _ptr(d_weight), int(accumulate),
+                                          _ptr(workspace), int(ws_bytes), _stream(stream)), "ec2moe_rmsnorm_backward")
 
 
 def ec2moe_activation(dtype, act, rows, cols, ld, U, V, perm, row_scale, H, stream=None):

@@ -145,6 +145,9 @@ def test_backward(rows, cols, dtype, y_dtype, with_dh):
     again, dw2 = torch.empty_like(dx), torch.empty_like(dw)
     call(dh, again, dw2)
     assert torch.equal(again, dx) and torch.equal(dw2, dw)
+    C.ec2moe_rmsnorm_backward(CODE[dtype], CODE[y_dtype], rows, cols, cols + 8, dy, h, rstd, w, dh, again, dw2, ws, ws.numel(),
+                              accumulate=1)
+    assert torch.equal(dw2, dw + dw)
     again.zero_()
     call(dh, again, None)
     assert torch.equal(again, dx)
@@ -185,4 +188,7 @@ def test_no_rows():
     dw = torch.full((64,), 3.0, device="cuda")
     C.ec2moe_rmsnorm_backward(C.BF16, C.BF16, 0, 64, 64, 0, 0, 0, 0, 0, 0, dw)
     assert bool((dw == 0).all())
+    dw.fill_(3.0)
+    C.ec2moe_rmsnorm_backward(C.BF16, C.BF16, 0, 64, 64, 0, 0, 0, 0, 0, 0, dw, accumulate=1)
+    assert bool((dw == 3).all())
     C.ec2moe_rmsnorm(C.BF16, C.BF16, 0, 64, 64, 0, 0, 0, 1e-5, 0, 0, 16)

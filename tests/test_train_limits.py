@@ -52,7 +52,7 @@ CASES = [
         (dict(dY=None), INVALID), (dict(H=None), INVALID), (dict(rstd=None), INVALID), (dict(dX=None), INVALID),
         (dict(cols=60), MISALIGNED), (dict(ld=68), MISALIGNED), (dict(cols=16392, ld=16392), UNSUPPORTED),
         (dict(dY=BAD), MISALIGNED), (dict(dH=BAD), MISALIGNED), (dict(weight=BAD), MISALIGNED), (dict(d_weight=BAD), MISALIGNED),
-        (dict(workspace=BAD), MISALIGNED), (dict(workspace=None), WORKSPACE), (dict(rows=0, d_weight=None), C.OK)]),
+        (dict(workspace=BAD), MISALIGNED), (dict(workspace=None), WORKSPACE), (dict(accumulate=2), INVALID), (dict(rows=0, d_weight=None), C.OK)]),
     (C.ec2moe_activation, ACT, [
         (dict(dtype=2), INVALID), (dict(act=2), INVALID), (dict(rows=-1), INVALID), (dict(ld=56), INVALID), (dict(U=None), INVALID),
         (dict(V=None), INVALID), (dict(H=None), INVALID), (dict(cols=60), MISALIGNED), (dict(ld=132), MISALIGNED),
