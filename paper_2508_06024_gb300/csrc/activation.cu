@@ -27,6 +27,33 @@ namespace {
 constexpr int PER = 8;
 constexpr int THREADS = 256;
 
+// 8 elements as they lie in memory: fetched ahead, widened when they are used.
+template <typename T>
+struct Raw8 {
+  U4 w[sizeof(T) / 2];
+};
+template <typename T>
+__device__ __forceinline__ Raw8<T> fetch8(const T* p) {
+  Raw8<T> r;
+#pragma unroll
+  for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) r.w[i] = reinterpret_cast<const U4*>(p)[i];
+  return r;
+}
+__device__ __forceinline__ void widen8(const Raw8<__nv_bfloat16>& r, float* v) {
+  const U4& q = r.w[0];
+  v[0] = bf16_lo(q.x); v[1] = bf16_hi(q.x); v[2] = bf16_lo(q.y); v[3] = bf16_hi(q.y);
+  v[4] = bf16_lo(q.z); v[5] = bf16_hi(q.z); v[6] = bf16_lo(q.w); v[7] = bf16_hi(q.w);
+}
+__device__ __forceinline__ void widen8(const Raw8<float>& r, float* v) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    v[4 * i + 0] = __uint_as_float(r.w[i].x);
+    v[4 * i + 1] = __uint_as_float(r.w[i].y);
+    v[4 * i + 2] = __uint_as_float(r.w[i].z);
+    v[4 * i + 3] = __uint_as_float(r.w[i].w);
+  }
+}
+
 __device__ __forceinline__ float sigmoid(float u) { return __fdividef(1.0f, 1.0f + __expf(-u)); }
 
 // The row's slot, or -1 (reported) where perm names none of the call's rows.
@@ -63,7 +90,7 @@ __global__ void __launch_bounds__(THREADS) activation_kernel(const ActArgs a, in
 }
 
 template <typename T, bool GLU>
-__global__ void __launch_bounds__(THREADS, 3) activation_backward_kernel(const ActArgs a, int tpr) {
+__global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 4 : 3) activation_backward_kernel(const ActArgs a, int tpr) {
   pdl_trigger();
   pdl_wait();
   __shared__ float s_sum[THREADS / 32];
@@ -80,12 +107,25 @@ __global__ void __launch_bounds__(THREADS, 3) activation_backward_kernel(const A
     T* du = static_cast<T*>(a.dU) + row * a.ld;
     T* dv = static_cast<T*>(a.dV) + row * a.ld;
     T* h = static_cast<T*>(a.H) + row * a.cols;
-#pragma unroll 2
+    // the next chunk's operands are on their way while this one's are used
+    Raw8<T> nu{}, nv{}, ng{};
+    if (t * PER < a.cols) {
+      nu = fetch8(u + t * PER);
+      if (GLU) nv = fetch8(v + t * PER);
+      ng = fetch8(dh + t * PER);
+    }
+#pragma unroll 1
     for (int c = t * PER; c < a.cols; c += tpr * PER) {
       float x[PER], y[PER], g[PER], o[PER];
-      load8(u + c, x);
-      if (GLU) load8(v + c, y);
-      load8(dh + c, g);
+      widen8(nu, x);
+      if (GLU) widen8(nv, y);
+      widen8(ng, g);
+      const int next = c + tpr * PER;
+      if (next < a.cols) {
+        nu = fetch8(u + next);
+        if (GLU) nv = fetch8(v + next);
+        ng = fetch8(dh + next);
+      }
 #pragma unroll
       for (int j = 0; j < PER; ++j) {
         const float gw = g[j] * w;
