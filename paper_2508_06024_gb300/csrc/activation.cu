@@ -5,7 +5,8 @@
 //
 // with s the gate weight of the row's slot.  SiLU(u) = u p with p = 1 / (1 + e^-u),
 // SiLU'(u) = p (1 + u (1 - p)); GELU(u) = u P(u) with P the normal distribution,
-// GELU'(u) = P(u) + u e^(-u^2 / 2) / sqrt(2 pi).  The gradient computes h again
+// GELU'(u) = P(u) + u e^(-u^2 / 2) / sqrt(2 pi).  P is taken from the fitted erfc of the 8-bit
+// experts (2.8e-8 at most, fp8.cuh): erff bound the kernel by its instructions.  The gradient computes h again
 // (the weights' gradient needs it, and it costs no read) and the gate weight's,
 // the row's sum of dh a.
 //
@@ -15,6 +16,7 @@
 #include <cuda_runtime.h>
 
 #include "common.cuh"
+#include "fp8.cuh"
 #include "internal.h"
 
 namespace ec2moe {
@@ -84,7 +86,7 @@ __global__ void __launch_bounds__(THREADS) activation_kernel(const ActArgs a, in
     load8(u + c, x);
     if (GLU) load8(v + c, y);
 #pragma unroll
-    for (int j = 0; j < PER; ++j) x[j] = GLU ? x[j] * sigmoid(x[j]) * y[j] * w : gelu_erf(x[j]) * w;
+    for (int j = 0; j < PER; ++j) x[j] = GLU ? x[j] * sigmoid(x[j]) * y[j] * w : gelu_fp8out(x[j]) * w;
     store8(h + c, x);
   }
 }
@@ -136,10 +138,11 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 4 : 3) activation_ba
           x[j] = gw * y[j] * (p * (1.0f + x[j] * (1.0f - p)));
           y[j] = gw * s;
         } else {
-          const float P = 0.5f * (1.0f + erff(x[j] * 0.70710678118654752f)), act = x[j] * P;
+          const float e = gauss(x[j]), tail = 0.5f * erfc_fit(fabsf(x[j]), e);
+          const float P = x[j] < 0.0f ? tail : 1.0f - tail, act = x[j] * P;
           sum = fmaf(g[j], act, sum);
           o[j] = act * w;
-          x[j] = gw * (P + x[j] * __expf(-0.5f * x[j] * x[j]) * 0.3989422804014327f);
+          x[j] = gw * (P + x[j] * e * 0.3989422804014327f);
         }
       }
       store8(du + c, x);

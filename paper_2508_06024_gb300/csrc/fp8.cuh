@@ -92,25 +92,34 @@ __device__ __forceinline__ U4 fp8_pack16(const float* v, float inv) {
   return U4{w[0], w[1], w[2], w[3]};
 }
 
-// GELU(u) = u Phi(u) = max(u, 0) - |u| erfc(|u| / sqrt 2) / 2 to fp32's own rounding:
-// erfc(x) = (c1 t + .. + c6 t^6) e^(-x^2), t = 1 / (1 + 0.4 x), the form of Abramowitz &
-// Stegun 7.1.26 with one term more, fitted here to the least largest error (Lawson's
-// weights): 2.8e-8, which with the roundings is 2.5e-7 at most.  Shorter forms move
+// erfc(x / sqrt 2) for x >= 0, with e = e^(-x^2 / 2) given: (c1 t + .. + c6 t^6) e, t = 1 /
+// (1 + 0.4 x / sqrt 2), the form of Abramowitz & Stegun 7.1.26 with one term more, fitted
+// here to the least largest error (Lawson's weights): 2.8e-8.
+__device__ __forceinline__ float erfc_fit(float x, float e) {
+  float t;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(fmaf(x, 0.4f * 0.70710678118654752f, 1.0f)));
+  float q = fmaf(t, -0.200259726f, 0.709149296f);
+  q = fmaf(t, q, -0.370911135f);
+  q = fmaf(t, q, 0.468276749f);
+  q = fmaf(t, q, 0.16182253f);
+  q = fmaf(t, q, 0.231922259f);
+  return q * t * e;
+}
+// e^(-u^2 / 2)
+__device__ __forceinline__ float gauss(float u) {
+  float e;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(u * u * (-0.5f * 1.4426950408889634f)));
+  return e;
+}
+// GELU(u) = u Phi(u) = max(u, 0) - |u| erfc(|u| / sqrt 2) / 2 to fp32's own rounding,
+// 2.5e-7 at most with the roundings.  Shorter forms move
 // hidden values over the e4m3 roundings' ties: with 7.1.28 (3e-7) fp32 experts of
 // 768 x 3072 were 6e-5 off (median of twelve inputs), with this and with the exact
 // form about 1e-5.  Half the exact
 // form's instructions (Switch sizes, 4096 rows: 56 us, 66).
 __device__ __forceinline__ float gelu_fp8out(float u) {
   const float x = fabsf(u);
-  float t, e;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(fmaf(x, 0.4f * 0.70710678118654752f, 1.0f)));
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(u * u * (-0.5f * 1.4426950408889634f)));
-  float q = fmaf(t, -0.200259726f, 0.709149296f);
-  q = fmaf(t, q, -0.370911135f);
-  q = fmaf(t, q, 0.468276749f);
-  q = fmaf(t, q, 0.16182253f);
-  q = fmaf(t, q, 0.231922259f);
-  return fmaf(-0.5f * x, q * t * e, fmaxf(u, 0.0f));
+  return fmaf(-0.5f * x, erfc_fit(x, gauss(u)), fmaxf(u, 0.0f));
 }
 
 namespace tc {

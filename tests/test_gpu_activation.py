@@ -1,9 +1,8 @@
 """The experts' activation with the gate weight, and its gradient, against 64 bits.
 
 Errors: SiLU and its derivative through fast exponentials, 2e-6 of themselves for the
-arguments here (|u| <= 12: e^|u| within |u| 2^-23 and 2 units of 2^-23, the quotient 2 units); erff is within
-2 units; a handful of roundings of 2^-24.  2e-6 of each term's magnitude covers them; GELU
-near its zeros on the left loses what 1 + erf cancels: 2^-23 |u|.
+arguments here (|u| <= 12: e^|u| within |u| 2^-23 and 2 units of 2^-23, the quotient 2 units); the normal
+distribution is within 3e-7; a handful of roundings of 2^-24.  2e-6 of each term's magnitude covers them.
 bf16 results are rounded by 2^-8.
 """
 import pytest
