@@ -19,17 +19,17 @@
 // CTA layout:
 //   warp 0       TMA producer
 //   warp 1       TMEM allocator and MMA issuer (the even CTA's)
-//   warp 2       (WGRAD) zeroes the sum rows of a stage behind the group's end
+//   warps 2, 3   (WGRAD) zero the sum rows of a stage behind the group's end
 //   16 warps     epilogue: warp w reads TMEM lanes 32 (w % 4) .. +31, every fourth
 //                block of 16 result rows
 //
 // Ragged sums (WGRAD): a group's last 64-row block may hold rows of the next
 // group, in both operands, and 0 times an infinity there would be NaN.  The MMAs
-// stop at the 16-row step that holds the last row, and warp 2 overwrites that
+// stop at the 16-row step that holds the last row, and warp 2 or 3 overwrites that
 // step's other rows with zeros once the block has landed, well before the MMAs
-// get to it: such a block completes on a barrier of its own (tland), and warp 2's
+// get to it: such a block completes on a barrier of its own (tland), and the warp's
 // arrival takes the place of the copies' on the stage's barrier.  The odd CTA's
-// warp 2 reports to the even one's (tpeer), which arrives for both.
+// warp reports to the even one's (tpeer), which arrives for both.
 //
 // Sums: the tensor core adds into its fp32 accumulator without rounding to
 // nearest, so sums are kept short: after `seg` blocks of 64 (8 for fp32 results, 128
@@ -75,8 +75,29 @@ constexpr int CHUNK = 64 * BK * 2;  // bytes of an MN-major chunk: 64 sum rows o
 constexpr int EPI_WARPS = 16;
 constexpr int MAX_GROUPS = 128;
 constexpr int BOX = 16;  // rows of the small box that short tiles' rows come in
+// Tiles along the rows that are walked together (16384 rows of 8 experts of 14336 x 4096,
+// gradient of the weights: 4 to 12 alike, 64 5% slower).
+constexpr int BAND = 8;
 
 enum Form { FWD = 0, DGRAD = 1, WGRAD = 2 };
+
+// n / d for 0 <= n < 2^31 by a multiplication: with m = ceil(2^(32 + s) / d), s = ceil(log2 d)
+// - 1, the quotient is floor(n m / 2^(32 + s)) (Granlund & Montgomery, 1994).  Every warp
+// takes four quotients per tile; as divisions they were most of a short tile's
+// instructions.
+struct FastDiv {
+  uint32_t m, s;
+  __device__ __forceinline__ int operator()(int n) const {
+    return m ? static_cast<int>(__umulhi(static_cast<uint32_t>(n), m) >> s) : n;
+  }
+};
+FastDiv fast_div(int d) {
+  if (d == 1) return FastDiv{0, 0};
+  uint32_t s = 0;
+  while ((1LL << (s + 1)) < d) ++s;
+  const uint64_t m = ((1ULL << (32 + s)) + d - 1) / d;
+  return FastDiv{static_cast<uint32_t>(m), s};
+}
 
 struct Params {
   const int32_t* offsets;  // [G + 1], nullptr: one group of all rows
@@ -85,7 +106,7 @@ struct Params {
   int out_rows;            // WGRAD: rows of a group's result
   int depth;               // FWD, DGRAD: length of the sums
   int tiles_c, tiles_r;    // tiles along the columns; WGRAD: along the rows
-  int band;                // tiles along the rows that are walked together
+  FastDiv by_split, by_group, by_band;  // ranges; WGRAD: tiles of a group; tiles of a band
   int split;               // ranges of the sum
   int seg;                 // blocks per segment
   const int32_t* perm;     // destination of each row (nullptr: itself); not with split > 1
@@ -129,13 +150,12 @@ struct Tile {
 template <int FORM>
 __device__ __forceinline__ Tile decode(const Params& p, int unit, const int* prefix, const int* cnt, int& cursor) {
   Tile t;
-  t.ks = unit % p.split;
-  int rem = unit / p.split;
+  int rem = p.by_split(unit);
+  t.ks = unit - rem * p.split;
   int tiles_r, n_rows;
   if (FORM == WGRAD) {
-    const int per = p.tiles_r * p.tiles_c;
-    t.g = rem / per;
-    rem -= t.g * per;
+    t.g = p.by_group(rem);
+    rem -= t.g * (p.tiles_r * p.tiles_c);
     tiles_r = p.tiles_r;
     n_rows = p.out_rows;
     t.len = cnt[t.g];
@@ -147,15 +167,15 @@ __device__ __forceinline__ Tile decode(const Params& p, int unit, const int* pre
     n_rows = cnt[t.g];
     t.len = p.depth;
   }
-  const int band = rem / (p.band * p.tiles_c);
-  const int wide = min(p.band, tiles_r - band * p.band);
-  rem -= band * p.band * p.tiles_c;
-  t.c = rem / wide;
-  t.r0 = (band * p.band + rem % wide) * BN;
+  const int band = p.by_band(rem);
+  const int wide = min(BAND, tiles_r - band * BAND);
+  rem -= band * (BAND * p.tiles_c);
+  t.c = wide == BAND ? rem / BAND : rem / wide;
+  t.r0 = (band * BAND + rem - t.c * wide) * BN;
   t.n = min(BN, n_rows - t.r0);
   t.nn = (t.n + 31) & ~31;
   const int n_kb = (t.len + BK - 1) / BK;
-  const int per_split = (n_kb + p.split - 1) / p.split;
+  const int per_split = p.by_split(n_kb + p.split - 1);
   t.kb0 = min(t.ks * per_split, n_kb);
   t.kb1 = min(t.kb0 + per_split, n_kb);
   return t;
@@ -413,10 +433,13 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         if (any && issue) sh.in_flight[2] = lane + 1;
       }
-    } else if (warp == 2) {
+    } else {
       if (FORM == WGRAD) {
         // ------------------------------------------------- rows behind a group's end
+        // The two warps take turns: a block's zeroes, fence and hand-over between the CTAs
+        // take about as long as a short unit.
         uint32_t blocks = 0;      // so far
+        uint32_t tails = 0;
         uint32_t tail_phase = 0;  // bit s: phase of stage s's tland and tpeer
         int cursor = 0;
         bool ok = true;
@@ -428,6 +451,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           const uint32_t stage = (blocks - 1) % STAGES, bit = 1u << stage;
           const uint32_t ph = (tail_phase & bit) ? 1u : 0u;
           tail_phase ^= bit;
+          if ((tails++ & 1u) != static_cast<uint32_t>(warp - 2)) continue;
           if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.tland[stage]), ph, budget, sh.abort_flag, &g_grouped_error))) {
             ok = false;
             break;
@@ -487,33 +511,53 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
       }
       float v[NB][16];
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[b][i] = 0.0f;
       bool ok = true;
-#pragma unroll 1
-      for (int s0 = t.kb0; s0 < t.kb1; s0 += p.seg, ++it) {
-        const uint32_t acc = it & 1u, acc_phase = (it >> 1) & 1u;
-        if (!__all_sync(0xffffffffu,
-                        mbar_wait_strict(smem_u32(&sh.tfull[acc]), acc_phase, budget, sh.abort_flag, &g_grouped_error))) {
-          ok = false;
-          break;
-        }
+      // the first segment comes straight into the sums, those behind it are added
+      auto arrived = [&] {
+        const bool here = __all_sync(0xffffffffu, mbar_wait_strict(smem_u32(&sh.tfull[it & 1u]), (it >> 1) & 1u, budget,
+                                                                   sh.abort_flag, &g_grouped_error));
         tc_fence_after();
-        const uint32_t at = tmem_base + acc * BN + (static_cast<uint32_t>(q * 32) << 16) + part * 16;
+        return here;
+      };
+      auto release = [&] {
+        tc_fence_before();
+        __syncwarp();
+        // both CTAs release the accumulator on the even CTA's barrier
+        if (lane == 0) mbar_arrive_remote(map_to_rank(smem_u32(&sh.tempty[it & 1u]), 0));
+        ++it;
+      };
+      const uint32_t lanes = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + part * 16;
+      if (t.kb0 < t.kb1) {
+        ok = arrived();
+        if (!ok) break;
+        uint32_t r[NB][16];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) tmem_ld16_nw(lanes + (it & 1u) * BN + b * 64, r[b]);
+        tmem_wait();
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[b][i] = __uint_as_float(r[b][i]);
+        release();
+      } else {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[b][i] = 0.0f;
+      }
+#pragma unroll 1
+      for (int s0 = t.kb0 + p.seg; s0 < t.kb1; s0 += p.seg) {
+        ok = arrived();
+        if (!ok) break;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
           uint32_t r[16];
-          tmem_ld16_nw(at + b * 64, r);
+          tmem_ld16_nw(lanes + (it & 1u) * BN + b * 64, r);
           tmem_wait();
 #pragma unroll
           for (int i = 0; i < 16; ++i) v[b][i] += __uint_as_float(r[i]);
         }
-        tc_fence_before();
-        __syncwarp();
-        // both CTAs release the accumulator on the even CTA's barrier
-        if (lane == 0) mbar_arrive_remote(map_to_rank(smem_u32(&sh.tempty[acc]), 0));
+        release();
       }
       if (!ok) break;
       const int col = t.c * 2 * BM + static_cast<int>(rank) * BM + q * 32 + lane;
@@ -772,8 +816,10 @@ cudaError_t launch(const GroupedArgs& a, int split, cudaStream_t s) {
   p.depth = FORM == FWD ? a.K : a.N;
   p.tiles_c = (p.cols + 2 * BM - 1) / (2 * BM);
   p.tiles_r = (a.N + BN - 1) / BN;
-  p.band = 8;
   p.split = split;
+  p.by_split = fast_div(split);
+  p.by_group = fast_div(p.tiles_r * p.tiles_c);
+  p.by_band = fast_div(BAND * p.tiles_c);
   p.seg = F32 ? 8 : 128;
   p.perm = parts ? nullptr : a.perm;
   p.out = parts ? a.workspace : a.out;
