@@ -119,17 +119,23 @@ struct Params {
 
 constexpr int A_BYTES = BM * BK * 2;      // M side per CTA and stage
 constexpr int B_BYTES = BN / 2 * BK * 2;  // N side, at most
-constexpr int STAGES = 7;
+constexpr int MAX_STAGES = 7;
+// bf16 results: the last stage's place is where they are transposed, two blocks of 16
+// rows x 64 bytes for every epilogue warp
+__host__ __device__ constexpr int stages(bool f32) { return f32 ? MAX_STAGES : MAX_STAGES - 1; }
+constexpr int STG_BLOCK = 16 * 64;
+constexpr int OFF_STG = (MAX_STAGES - 1) * (A_BYTES + B_BYTES);
+static_assert(2 * EPI_WARPS * STG_BLOCK <= A_BYTES + B_BYTES, "the blocks take the place of a stage");
 constexpr int TMEM_COLS = 2 * BN;
-// full, empty, tland, tpeer [STAGES]; tfull, tempty [2]; drain
-constexpr int N_BARS = 4 * STAGES + 5;
-constexpr int OFF_BARS = STAGES * (A_BYTES + B_BYTES);
+// full, empty, tland, tpeer [MAX_STAGES]; tfull, tempty [2]; drain
+constexpr int N_BARS = 4 * MAX_STAGES + 5;
+constexpr int OFF_BARS = MAX_STAGES * (A_BYTES + B_BYTES);
 constexpr int OFF_SLOT = OFF_BARS + N_BARS * 8;
 constexpr int OFF_PREFIX = OFF_SLOT + 24;
 constexpr int OFF_ROW0 = OFF_PREFIX + (MAX_GROUPS + 1) * 4;
 constexpr int OFF_CNT = OFF_ROW0 + MAX_GROUPS * 4;
 constexpr int SMEM = 1024 + OFF_CNT + MAX_GROUPS * 4;
-static_assert(STAGES <= 16 && OFF_BARS % 8 == 0 && SMEM <= 232448, "shared memory per CTA");
+static_assert(MAX_STAGES <= 16 && OFF_BARS % 8 == 0 && SMEM <= 232448, "shared memory per CTA");
 constexpr int FIRST_EPI = 4;  // the first warpgroup loads, issues and zeroes
 constexpr int THREADS = 32 * (FIRST_EPI + EPI_WARPS);
 // Registers: 640 threads start with 96 each (61440); the epilogue takes what the first
@@ -206,6 +212,22 @@ __device__ __forceinline__ void arrive_cluster(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 
+// 16 TMEM lanes x 16 columns of 32-bit words, issue only: thread t receives, for each 8
+// columns, those at 2 (t % 4) and the next of lane t / 4 and of lane t / 4 + 8: the layout
+// of an 8 x 8 matrix's fragments.
+__device__ __forceinline__ void tmem_ld_16x16_nw(uint32_t taddr, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr));
+}
+// Four 8 x 8 matrices of 16-bit elements, stored transposed: thread t names row t % 8 of
+// matrix t / 8 (16 bytes).
+__device__ __forceinline__ void store_4_transposed(uint32_t saddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(saddr), "r"(a), "r"(b), "r"(c),
+               "r"(d)
+               : "memory");
+}
+
 // What the roles share.
 struct Shared {
   uint8_t *sA, *sB;
@@ -231,6 +253,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                         const __grid_constant__ CUtensorMap tmBox, const Params p) {
   constexpr bool A_MN = FORM != FWD, B_MN = FORM == WGRAD;
+  constexpr int STAGES = stages(F32);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   Shared sh;
@@ -484,29 +507,41 @@ __global__ void __launch_bounds__(THREADS, 1)
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_EPI));
     // ---------------------------------------------------------------- epilogue
-    // A thread's result column is its TMEM lane; its rows are the blocks of 16
-    // part, part + 4, part + 8, part + 12.
+    // A warp has 32 result columns (its TMEM lanes) and the blocks of 16 rows part, part +
+    // 4, part + 8, part + 12.  fp32: a thread's column is its TMEM lane.  bf16: fragments of
+    // 8 x 8 matrices, 8 columns by 8 rows.
     const int q = warp & 3;
     const int part = (warp - FIRST_EPI) >> 2;
     constexpr int NB = BN / 64;  // blocks of a warp
     using OutT = typename std::conditional<F32, float, __nv_bfloat16>::type;
     uint32_t it = 0;
     int cursor = 0;
+    auto load_block = [&](uint32_t lanes, int b, uint32_t* r) {
+      if constexpr (F32) {
+        tmem_ld16_nw(lanes + b * 64, r);
+      } else {
+        tmem_ld_16x16_nw(lanes + b * 64, r);
+        tmem_ld_16x16_nw(lanes + b * 64 + (16u << 16), r + 8);
+      }
+    };
     for (int unit = unit_first; unit < n_units; unit += unit_step) {
       const Tile t = decode<FORM>(p, unit, sh.prefix, sh.cnt, cursor);
       if (t.kb0 >= t.kb1 && (FORM != WGRAD || p.split > 1 || p.accumulate)) continue;  // nothing to add
-      // With a perm, lane l: destinations of the rows l % 16 of the warp's blocks l / 16 and
-      // 2 + l / 16 (-1: none).  Without, the tile's rows follow each other.
-      int dst[2];
       const int first = FORM == WGRAD ? t.r0 : sh.row0[t.g] + t.r0;
+      // With a perm: destinations (-1: none).  fp32: lane l those of the rows l % 16 of the
+      // warp's blocks l / 16 and 2 + l / 16.  bf16: of the rows l / 4 and 8 + l / 4 of each block.
+      int dst[NB][2];
       if constexpr (PERM) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int r = (part + 4 * (2 * h + (lane >> 4))) * 16 + (lane & 15);
-          dst[h] = r < t.n ? p.perm[first + r] : -1;
-          if (r < t.n && (dst[h] < 0 || dst[h] >= p.rows)) {
-            atomicOr(&g_grouped_error, 2u);
-            dst[h] = -1;
+        for (int b = 0; b < (F32 ? 1 : NB); ++b) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int r = F32 ? (part + 4 * (2 * h + (lane >> 4))) * 16 + (lane & 15) : (part + 4 * b) * 16 + 8 * h + (lane >> 2);
+            dst[b][h] = r < t.n ? p.perm[first + r] : -1;
+            if (r < t.n && (dst[b][h] < 0 || dst[b][h] >= p.rows)) {
+              atomicOr(&g_grouped_error, 2u);
+              dst[b][h] = -1;
+            }
           }
         }
       }
@@ -532,7 +567,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (!ok) break;
         uint32_t r[NB][16];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) tmem_ld16_nw(lanes + (it & 1u) * BN + b * 64, r[b]);
+        for (int b = 0; b < NB; ++b) load_block(lanes + (it & 1u) * BN, b, r[b]);
         tmem_wait();
 #pragma unroll
         for (int b = 0; b < NB; ++b)
@@ -552,7 +587,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
           uint32_t r[16];
-          tmem_ld16_nw(lanes + (it & 1u) * BN + b * 64, r);
+          load_block(lanes + (it & 1u) * BN, b, r);
           tmem_wait();
 #pragma unroll
           for (int i = 0; i < 16; ++i) v[b][i] += __uint_as_float(r[i]);
@@ -560,40 +595,26 @@ __global__ void __launch_bounds__(THREADS, 1)
         release();
       }
       if (!ok) break;
-      const int col = t.c * 2 * BM + static_cast<int>(rank) * BM + q * 32 + lane;
-      const bool held = col < p.cols;
-      const int odd = F32 ? 0 : lane & 1;
-      // where this lane's column (bf16: pair of columns) of row 0 lies
-      OutT* out = static_cast<OutT*>(p.out) + t.ks * p.part_stride + (col - odd);
-      if (FORM == WGRAD) out += static_cast<long long>(t.g) * p.out_rows * p.ldo;
-      // bf16: two rows at a time, even lanes the first and the column beside theirs, odd
-      // lanes the second (the two halves of the lane's packed pair and its neighbour's)
-      const uint32_t pick = odd ? 0x3276u : 0x5410u;
-      if constexpr (PERM) {
+      const int col0 = t.c * 2 * BM + static_cast<int>(rank) * BM + q * 32;
+      if constexpr (F32) {
+        const int col = col0 + lane;
+        const bool held = col < p.cols;
+        float* out = static_cast<float*>(p.out) + t.ks * p.part_stride + col;
+        if (FORM == WGRAD) out += static_cast<long long>(t.g) * p.out_rows * p.ldo;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
           if ((part + 4 * b) * 16 >= t.n) break;  // the whole warp
+          // a row of the warp: 128 contiguous bytes
+          if constexpr (PERM) {
 #pragma unroll
-          for (int i = 0; i < 16; i += F32 ? 1 : 2) {
-            const int d = __shfl_sync(0xffffffffu, dst[b >> 1], (b & 1) * 16 + i + odd);
-            if constexpr (F32) {
+            for (int i = 0; i < 16; ++i) {
+              const int d = __shfl_sync(0xffffffffu, dst[0][b >> 1], (b & 1) * 16 + i);
               if (d >= 0 && held) out[d * p.ldo] = v[b][i];
-            } else {
-              const uint32_t w = pack_bf16x2(v[b][i], v[b][i + 1]);
-              const uint32_t o = __byte_perm(w, __shfl_xor_sync(0xffffffffu, w, 1), pick);
-              if (d >= 0 && held) *reinterpret_cast<uint32_t*>(out + d * p.ldo) = o;
             }
+            continue;
           }
-        }
-        continue;
-      }
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        if ((part + 4 * b) * 16 >= t.n) break;  // the whole warp
-        OutT* to = out + (first + (part + 4 * b) * 16 + odd) * p.ldo;
-        const int n = held ? t.n - (part + 4 * b) * 16 - odd : 0;
-        if constexpr (F32) {
-          // a row of the warp: 128 contiguous bytes; four rows at a time
+          float* to = out + (first + (part + 4 * b) * 16) * p.ldo;
+          const int n = held ? t.n - (part + 4 * b) * 16 : 0;
 #pragma unroll
           for (int i = 0; i < 16; i += 4, to += 4 * p.ldo) {
             if (FORM == WGRAD && p.accumulate) {
@@ -607,14 +628,43 @@ __global__ void __launch_bounds__(THREADS, 1)
             for (int j = 0; j < 4; ++j)
               if (i + j < n) to[j * p.ldo] = v[b][i + j];
           }
-        } else {
+        }
+      } else {
+        // A block of 16 rows x 32 columns is transposed through shared memory (rows of 64
+        // bytes, their 16-byte pieces permuted so that no side meets a bank twice) and
+        // stored 8 rows at a time, 16 bytes per lane.  Packed in registers and stored two
+        // columns per lane, a tile took 600 instructions per warp: 211 us for 256 rows of 8
+        // experts of 14336 x 4096.
+        const uint32_t stg = smem_u32(smem + OFF_STG) + (warp - FIRST_EPI) * 2 * STG_BLOCK;
+        const uint32_t put = stg + (lane & 7) * 64 + (((lane >> 3) ^ ((lane >> 1) & 3)) * 16);
+        const uint32_t get = stg + (lane >> 2) * 64 + (((lane & 3) ^ ((lane >> 3) & 3)) * 16);
+        const bool held = col0 + (lane & 3) * 8 < p.cols;
+        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + col0 + (lane & 3) * 8;
+        if (FORM == WGRAD) out += static_cast<long long>(t.g) * p.out_rows * p.ldo;
 #pragma unroll
-          for (int i = 0; i < 16; i += 2, to += 2 * p.ldo) {
-            const uint32_t w = pack_bf16x2(v[b][i], v[b][i + 1]);
-            const uint32_t o = __byte_perm(w, __shfl_xor_sync(0xffffffffu, w, 1), pick);
-            if (i < n) *reinterpret_cast<uint32_t*>(to) = o;
+        for (int b = 0; b < NB; ++b) {
+          if ((part + 4 * b) * 16 >= t.n) break;  // the whole warp
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {  // 8 rows each
+            const float* f = v[b] + 4 * k;
+            store_4_transposed(put + (b & 1) * STG_BLOCK + k * 512, pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]),
+                               pack_bf16x2(f[8], f[9]), pack_bf16x2(f[10], f[11]));
+          }
+          __syncwarp();
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int r = (part + 4 * b) * 16 + 8 * h + (lane >> 2);
+            U4 o;
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(o.x), "=r"(o.y), "=r"(o.z), "=r"(o.w)
+                         : "r"(get + (b & 1) * STG_BLOCK + h * 512)
+                         : "memory");
+            const bool on = held && (PERM ? dst[b][h] >= 0 : r < t.n);
+            const long long d = PERM ? dst[b][h] : first + r;
+            if (on) *reinterpret_cast<U4*>(out + d * p.ldo) = o;
           }
         }
+        __syncwarp();
       }
     }
   }
