@@ -459,10 +459,11 @@ __global__ void __launch_bounds__(THREADS, 1)
     } else {
       if (FORM == WGRAD) {
         // ------------------------------------------------- rows behind a group's end
-        // The two warps take turns: a block's zeroes, fence and hand-over between the CTAs
-        // take about as long as a short unit.
+        // The two warps share the stages, even and odd ones: a block's zeroes, fence and
+        // hand-over between the CTAs take about as long as a short unit.  Every such block of
+        // a stage is one warp's, so that it has seen a phase of the stage's barriers before the
+        // next one can begin: a phase's parity alone does not tell it from the one before.
         uint32_t blocks = 0;      // so far
-        uint32_t tails = 0;
         uint32_t tail_phase = 0;  // bit s: phase of stage s's tland and tpeer
         int cursor = 0;
         bool ok = true;
@@ -472,9 +473,9 @@ __global__ void __launch_bounds__(THREADS, 1)
           const int left = t.len - (t.kb1 - 1) * BK;
           if (t.kb1 <= t.kb0 || left >= BK || left % UK == 0) continue;
           const uint32_t stage = (blocks - 1) % STAGES, bit = 1u << stage;
+          if ((stage & 1u) != static_cast<uint32_t>(warp - 2)) continue;
           const uint32_t ph = (tail_phase & bit) ? 1u : 0u;
           tail_phase ^= bit;
-          if ((tails++ & 1u) != static_cast<uint32_t>(warp - 2)) continue;
           if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.tland[stage]), ph, budget, sh.abort_flag, &g_grouped_error))) {
             ok = false;
             break;

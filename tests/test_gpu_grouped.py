@@ -168,6 +168,21 @@ def test_no_rows():
     assert bool((out == 0).all())
 
 
+@pytest.mark.parametrize("out_type", [C.BF16, C.F32])
+@pytest.mark.parametrize("lengths", [[379, 379, 379], [443, 443, 443], [379, 384, 320, 443, 448, 379], [5, 64, 3, 128, 9, 0, 70, 2048, 1921]])
+def test_ragged_sums_of_many_tiles(lengths, out_type):
+    """Several tiles per CTA pair, each sum ending inside a block, with as many blocks as the pipeline has
+    stages (6, 7) or with whole sums in between: blocks that end a sum come to the same stage one after the other."""
+    offsets = [0]
+    for n in lengths:
+        offsets.append(offsets[-1] + n)
+    G, rows, N, K = len(lengths), offsets[-1], 3000, 2560
+    X, W = operands("wgrad", rows, N, K, G, seed=14)
+    for _ in range(2):
+        out = call("wgrad", X, W, offsets, G, rows, N, K, out_type)
+        check("wgrad", X, W, offsets, G, rows, N, K, out, out_type)
+
+
 @pytest.mark.parametrize("form", FORMS)
 def test_other_groups_values_stay_out(form):
     """Infinities and NaN in one group's rows, and in rows of no group, reach no other group's results."""
