@@ -37,8 +37,10 @@
 // the epilogue, while the next segment fills the other one.
 //
 // Split sums: where there are fewer tiles than CTA pairs the sum is cut into
-// ranges; each writes fp32 partial results to the workspace and a second kernel
-// adds them in order.
+// ranges.  Up to 4 are a cluster's pairs (CLUSTER): each pair leaves its sums where its
+// operands were, and after a cluster barrier every pair adds up its share of the
+// rows through distributed shared memory, in the order of the ranges.  More ranges
+// write fp32 partial results to the workspace and a second kernel adds them in order.
 //
 // Every wait is bounded: a wait that gives up sets the error word and the CTA's
 // abort flag, waits for copies and MMAs in flight, frees its tensor memory and
@@ -108,9 +110,10 @@ struct Params {
   int tiles_c, tiles_r;    // tiles along the columns; WGRAD: along the rows
   FastDiv by_split, by_group, by_band;  // ranges; WGRAD: tiles of a group; tiles of a band
   int split;               // ranges of the sum
+  int out_bf16;            // CLUSTER: type of the result
   int seg;                 // blocks per segment
-  const int32_t* perm;     // destination of each row (nullptr: itself); not with split > 1
-  void* out;               // split > 1: fp32 [split][...], dense
+  const int32_t* perm;     // destination of each row (nullptr: itself); not with ranges in the workspace
+  void* out;               // ranges in the workspace: fp32 [split][...], dense
   long long ldo;
   long long part_stride;   // elements between two ranges' partial results
   int accumulate;
@@ -136,6 +139,8 @@ constexpr int OFF_ROW0 = OFF_PREFIX + (MAX_GROUPS + 1) * 4;
 constexpr int OFF_CNT = OFF_ROW0 + MAX_GROUPS * 4;
 constexpr int SMEM = 1024 + OFF_CNT + MAX_GROUPS * 4;
 static_assert(MAX_STAGES <= 16 && OFF_BARS % 8 == 0 && SMEM <= 232448, "shared memory per CTA");
+constexpr int MAX_PAIRS = 4;  // of a cluster
+static_assert(BN * BM * 4 <= OFF_BARS, "the sums take the operands' place");
 constexpr int FIRST_EPI = 4;  // the first warpgroup loads, issues and zeroes
 constexpr int THREADS = 32 * (FIRST_EPI + EPI_WARPS);
 // Registers: 640 threads start with 96 each (61440); the epilogue takes what the first
@@ -228,6 +233,15 @@ __device__ __forceinline__ void store_4_transposed(uint32_t saddr, uint32_t a, u
                : "memory");
 }
 
+// Arrives on the barrier at shared address `bar` in both CTAs of the pair whose even CTA
+// has rank `lead` in the cluster, once the pair's MMAs issued so far have completed.
+__device__ __forceinline__ void commit_to_pair(uint32_t bar, uint32_t lead) {
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+      "h"(static_cast<uint16_t>(0x3u << lead))
+      : "memory");
+}
+
 // What the roles share.
 struct Shared {
   uint8_t *sA, *sB;
@@ -248,7 +262,61 @@ __device__ __forceinline__ void scan_groups(const Params& p, int lane, const Sha
   warp_exclusive_scan<CHUNKS>(p.G, lane, [&](int g) { return (sh.cnt[g] + BN - 1) / BN; }, sh.prefix);
 }
 
-template <int FORM, bool F32, bool PERM>
+template <int FORM>
+__device__ __forceinline__ Tile decode_any(const Params& p, int unit, const int* prefix, const int* cnt) {
+  int cursor = 0;
+  return decode<FORM>(p, unit, prefix, cnt, cursor);
+}
+
+// CLUSTER: this CTA's columns of its pair's share of the tile's rows, from the sums that
+// the pairs' CTAs of the same rank left at `sums` ([row][BM] fp32).  A warp takes a row.
+template <int FORM>
+__device__ __forceinline__ void join_ranges(const Params& p, const Tile& t, const Shared& sh, uint32_t sums, uint32_t cta) {
+  const int warp = (threadIdx.x >> 5) - FIRST_EPI, lane = threadIdx.x & 31;
+  const int piece = static_cast<int>(cta >> 1), share = (t.n + p.split - 1) / p.split;
+  const int end = min(t.n, (piece + 1) * share);
+  const int col = (t.c * 2 + static_cast<int>(cta & 1u)) * BM + lane * 4;
+  uint32_t from[MAX_PAIRS];
+#pragma unroll
+  for (int s = 0; s < MAX_PAIRS; ++s) from[s] = map_to_rank(sums, s < p.split ? 2 * s + (cta & 1u) : cta) + lane * 16;
+  for (int r = piece * share + warp; r < end; r += EPI_WARPS) {
+    long long d = t.r0 + r;
+    if (FORM == WGRAD) {
+      d += static_cast<long long>(t.g) * p.out_rows;
+    } else {
+      d += sh.row0[t.g];
+      if (p.perm) {
+        d = p.perm[d];
+        if (d < 0 || d >= p.rows) {
+          if (lane == 0) atomicOr(&g_grouped_error, 2u);
+          continue;
+        }
+      }
+    }
+    float4 x[MAX_PAIRS];
+#pragma unroll
+    for (int s = 0; s < MAX_PAIRS; ++s)
+      if (s < p.split) x[s] = ld_cluster_v4(from[s] + r * (BM * 4));
+    float4 v = x[0];
+#pragma unroll
+    for (int s = 1; s < MAX_PAIRS; ++s)
+      if (s < p.split) v = make_float4(v.x + x[s].x, v.y + x[s].y, v.z + x[s].z, v.w + x[s].w);
+    if (col >= p.cols) continue;
+    if (p.out_bf16) {
+      *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + d * p.ldo + col) =
+          make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+    } else {
+      float4* to = reinterpret_cast<float4*>(static_cast<float*>(p.out) + d * p.ldo + col);
+      if (FORM == WGRAD && p.accumulate) {
+        const float4 o = *to;
+        v = make_float4(v.x + o.x, v.y + o.y, v.z + o.z, v.w + o.w);
+      }
+      *to = v;
+    }
+  }
+}
+
+template <int FORM, bool F32, bool PERM, bool CLUSTER>
 __global__ void __launch_bounds__(THREADS, 1)
     grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                         const __grid_constant__ CUtensorMap tmBox, const Params p) {
@@ -275,9 +343,13 @@ __global__ void __launch_bounds__(THREADS, 1)
 
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
-  const uint32_t rank = cluster_ctarank();
-  const int unit_first = static_cast<int>(cluster_id_x());
-  const int unit_step = static_cast<int>(cluster_count_x());
+  static_assert(!CLUSTER || (F32 && !PERM), "the ranges' sums are fp32 and have their own way out");
+  // Rank in the CTA pair, the even CTA's rank in the cluster.  CLUSTER: the cluster has one
+  // tile, or none, and each of its pairs a range.
+  const uint32_t cta = cluster_ctarank();
+  const uint32_t rank = cta & 1u, lead = CLUSTER ? cta & ~1u : 0u;
+  const int unit_first = static_cast<int>(cluster_id_x()) * (CLUSTER ? p.split : 1) + (CLUSTER ? static_cast<int>(cta >> 1) : 0);
+  const int unit_step = CLUSTER ? 1 << 29 : static_cast<int>(cluster_count_x());
   pdl_trigger();
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
@@ -357,7 +429,7 @@ __global__ void __launch_bounds__(THREADS, 1)
               uint32_t bar = smem_u32(&sh.full[stage]);
               // both CTAs' copies complete on the even CTA's barrier
               if (rank == 0) mbar_expect_tx(bar, 2 * (A_BYTES + b_bytes));
-              else bar = map_to_rank(bar, 0);
+              else bar = map_to_rank(bar, lead);
               if (FORM == WGRAD) {
 #pragma unroll
                 for (int c = 0; c < BM / 64; ++c) tma_load_2d_to_pair_bar(da + c * CHUNK, &tmA, c0 + c * 64, row0 + k0, bar);
@@ -443,7 +515,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                   if (FORM == WGRAD && kk * UK >= left) break;
                   umma_bf16_pair(d, da + kk * STEP_A, db + kk * STEP_B, idesc, kb != s0 || kk != 0 ? 1u : 0u);
                 }
-                umma_commit_pair_mc(smem_u32(&sh.empty[stage]));
+                commit_to_pair(smem_u32(&sh.empty[stage]), lead);
               }
               any = true;
               if (++stage == STAGES) {
@@ -451,7 +523,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                 phase ^= 1u;
               }
             }
-            if (ok && issue) umma_commit_pair_mc(smem_u32(&sh.tfull[acc]));
+            if (ok && issue) commit_to_pair(smem_u32(&sh.tfull[acc]), lead);
           }
         }
         if (any && issue) sh.in_flight[2] = lane + 1;
@@ -493,7 +565,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           asm volatile("fence.proxy.async;" ::: "memory");
           __syncwarp();
           if (rank != 0) {
-            if (lane == 0) arrive_cluster(map_to_rank(smem_u32(&sh.tpeer[stage]), 0));
+            if (lane == 0) arrive_cluster(map_to_rank(smem_u32(&sh.tpeer[stage]), lead));
             continue;
           }
           if (!__all_sync(0xffffffffu,
@@ -527,7 +599,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     };
     for (int unit = unit_first; unit < n_units; unit += unit_step) {
       const Tile t = decode<FORM>(p, unit, sh.prefix, sh.cnt, cursor);
-      if (t.kb0 >= t.kb1 && (FORM != WGRAD || p.split > 1 || p.accumulate)) continue;  // nothing to add
+      if (!CLUSTER && t.kb0 >= t.kb1 && (FORM != WGRAD || p.split > 1 || p.accumulate)) continue;  // nothing to add
       const int first = FORM == WGRAD ? t.r0 : sh.row0[t.g] + t.r0;
       // With a perm: destinations (-1: none).  fp32: lane l those of the rows l % 16 of the
       // warp's blocks l / 16 and 2 + l / 16.  bf16: of the rows l / 4 and 8 + l / 4 of each block.
@@ -559,7 +631,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         tc_fence_before();
         __syncwarp();
         // both CTAs release the accumulator on the even CTA's barrier
-        if (lane == 0) mbar_arrive_remote(map_to_rank(smem_u32(&sh.tempty[it & 1u]), 0));
+        if (lane == 0) mbar_arrive_remote(map_to_rank(smem_u32(&sh.tempty[it & 1u]), lead));
         ++it;
       };
       const uint32_t lanes = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + part * 16;
@@ -597,7 +669,16 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
       if (!ok) break;
       const int col0 = t.c * 2 * BM + static_cast<int>(rank) * BM + q * 32;
-      if constexpr (F32) {
+      if constexpr (CLUSTER) {
+        // the operands' place is free: the last MMAs have read them
+        float* sums = reinterpret_cast<float*>(smem) + q * 32 + lane;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          if ((part + 4 * b) * 16 >= t.n) break;  // the whole warp
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sums[((part + 4 * b) * 16 + i) * BM] = v[b][i];
+        }
+      } else if constexpr (F32) {
         const int col = col0 + lane;
         const bool held = col < p.cols;
         float* out = static_cast<float*>(p.out) + t.ks * p.part_stride + col;
@@ -675,7 +756,15 @@ __global__ void __launch_bounds__(THREADS, 1)
   // the even CTA's MMAs read both CTAs' shared memory and write both CTAs' TMEM;
   // neither is released before both CTAs are done with them, nor, where a wait of either
   // gave up, before what is in flight has ended
-  if (threadIdx.x == 0) abort_pair(sh.abort_flag, rank);
+  if (CLUSTER) {
+    // all of the cluster agree: they meet at further barriers
+    if (threadIdx.x < 2 * p.split && threadIdx.x != cta && *sh.abort_flag)
+      asm volatile("st.shared::cluster.s32 [%0], 1;" ::"r"(
+                       map_to_rank(smem_u32(const_cast<int*>(sh.abort_flag)), threadIdx.x))
+                   : "memory");
+  } else if (threadIdx.x == 0) {
+    abort_pair(sh.abort_flag, rank);
+  }
   __syncwarp();
   cluster_sync_all();
   if (*sh.abort_flag) {  // no warp waits any more: the same in all of them, and in the pair
@@ -690,6 +779,12 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_drain(smem_u32(sh.drain), 0, DRAIN_CYCLES);
     }
     __syncthreads();
+    __syncwarp();
+    cluster_sync_all();
+  } else if (CLUSTER && warp >= FIRST_EPI && unit_first < n_units) {
+    join_ranges<FORM>(p, decode_any<FORM>(p, unit_first, sh.prefix, sh.cnt), sh, smem_u32(smem), cta);
+  }
+  if (CLUSTER) {  // no CTA ends while another reads its sums
     __syncwarp();
     cluster_sync_all();
   }
@@ -798,14 +893,29 @@ bool encode(CUtensorMap* m, const void* ptr, int mats, long long rows, long long
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Into how many ranges a call's sums are cut: the least of
-//   waves(tiles * S) * blocks of a range * 0.27 us, or what HBM needs if that is more,
-//   + for S > 1: 4.6 us and the partial results' way to the workspace and back
+// How a call's sums are cut.
+struct Plan {
+  int split;     // ranges
+  bool cluster;  // the pairs of a cluster each
+};
+
+template <int FORM>
+int clusters_of(int split) {
+  auto kernel = grouped_gemm_kernel<FORM, true, false, true>;
+  const void* kfn = reinterpret_cast<const void*>(kernel);
+  return ensure_smem_attr(kfn, SMEM) == cudaSuccess ? max_clusters(kfn, THREADS, SMEM, 2 * split) : 0;
+}
+
+// The least of
+//   waves * blocks of a range * 0.27 us, or what HBM needs if that is more,
+//   + for ranges in a cluster 2 us, for ranges in the workspace 4.6 us and the partial
+//   results' way there and back
 // (0.27 us: a block of 64 of one tile at full clock; the others fitted to 700 x 512 x
-// 4096: one range 27 us, four 19, seven 17; 700 x 4096 x 4096: 27, two 41; the gradient
-// of 512 x 4096 weights over 8191 rows: 48, two 40, four 45; 32 rows of 8 experts of 4096
-// x 14336, bound by HBM: 139, two 160).  Ragged rows: the tiles are expected ones.
-int split_of(int form, int G, int rows, int N, int K) {
+// 4096 in the workspace: one range 27 us, four 19, seven 17; 700 x 4096 x 4096: 27, two 41;
+// the gradient of 512 x 4096 weights over 8191 rows: 48, two 40, four 45; 32 rows of 8
+// experts of 4096 x 14336, bound by HBM: 139, two 160).  Ragged rows: the tiles are
+// expected ones.
+Plan plan_of(int form, int G, int rows, int N, int K) {
   const int pairs = sm_count() / 2;
   const int cols = form == FWD ? N : K;
   const double tiles_c = (cols + 2 * BM - 1) / (2 * BM);
@@ -824,25 +934,31 @@ int split_of(int form, int G, int rows, int N, int K) {
     bytes = 2.0 * rows * (static_cast<double>(N) + K) + 2.0 * held * N * static_cast<double>(K);
   }
   const double hbm = bytes / 6.4e6;  // us
-  int best = 1;
+  Plan best{1, false};
   double least = 0.0;
   for (int s = 1; s <= GROUPED_MAX_SPLIT && (s == 1 || s * 4 <= n_kb); ++s) {
     const int per = (n_kb + s - 1) / s;
     if ((n_kb + per - 1) / per != s) continue;  // no empty range (FWD, DGRAD)
-    const double waves = ceil(tiles * s / pairs);
-    const double mma = waves * per * 0.27;
-    const double us = (mma > hbm ? mma : hbm) + (s > 1 ? 4.6 + s * out * 8.0 / 5e6 : 0.0);
-    if (s == 1 || us < least) {
-      best = s;
-      least = us;
+    for (int cluster = 0; cluster < 2; ++cluster) {
+      if (cluster && (s == 1 || s > MAX_PAIRS || tiles * s > pairs)) continue;
+      int at_once = pairs / s;
+      if (cluster) at_once = form == FWD ? clusters_of<FWD>(s) : form == DGRAD ? clusters_of<DGRAD>(s) : clusters_of<WGRAD>(s);
+      if (cluster && at_once < 1) continue;
+      const double waves = cluster ? ceil(tiles / at_once) : ceil(tiles * s / pairs);
+      const double mma = waves * per * 0.27;
+      const double us = (mma > hbm ? mma : hbm) + (s == 1 ? 0.0 : cluster ? 2.0 : 4.6 + s * out * 8.0 / 5e6);
+      if (least == 0.0 || us < least) {
+        best = Plan{s, cluster != 0};
+        least = us;
+      }
     }
   }
   return best;
 }
 
-template <int FORM, bool F32, bool PERM>
+template <int FORM, bool F32, bool PERM, bool CLUSTER>
 cudaError_t launch(const GroupedArgs& a, int split, cudaStream_t s) {
-  auto kernel = grouped_gemm_kernel<FORM, F32, PERM>;
+  auto kernel = grouped_gemm_kernel<FORM, F32, PERM, CLUSTER>;
   const void* kfn = reinterpret_cast<const void*>(kernel);
   cudaError_t e = ensure_smem_attr(kfn, SMEM);
   if (e != cudaSuccess) return e;
@@ -857,7 +973,7 @@ cudaError_t launch(const GroupedArgs& a, int split, cudaStream_t s) {
            encode(&mB, a.X, 0, a.rows, depth, a.ldx, BN / 2) && encode(&mBox, a.X, 0, a.rows, depth, a.ldx, BOX);
   }
   if (!good) return cudaErrorInvalidValue;
-  const bool parts = split > 1;
+  const bool parts = split > 1 && !CLUSTER;
   Params p{};
   p.offsets = a.offsets;
   p.G = a.G;
@@ -871,6 +987,7 @@ cudaError_t launch(const GroupedArgs& a, int split, cudaStream_t s) {
   p.by_split = fast_div(split);
   p.by_group = fast_div(p.tiles_r * p.tiles_c);
   p.by_band = fast_div(BAND * p.tiles_c);
+  p.out_bf16 = a.out_bf16;
   p.seg = F32 ? 8 : 128;
   p.perm = parts ? nullptr : a.perm;
   p.out = parts ? a.workspace : a.out;
@@ -880,12 +997,17 @@ cudaError_t launch(const GroupedArgs& a, int split, cudaStream_t s) {
   p.timeout = a.timeout_cycles;
   const long long row_tiles = FORM == WGRAD ? static_cast<long long>(a.G) * p.tiles_r : a.rows / BN + a.G;
   const long long units = row_tiles * p.tiles_c * p.split;
-  int clusters = max_clusters(kfn, THREADS, SMEM, 2);
-  if (clusters < 1) return cudaErrorInvalidConfiguration;
-  if (units < clusters) clusters = static_cast<int>(units);
+  int clusters;
+  if (CLUSTER) {
+    clusters = static_cast<int>(units / split);  // one tile each, at most
+  } else {
+    clusters = max_clusters(kfn, THREADS, SMEM, 2);
+    if (clusters < 1) return cudaErrorInvalidConfiguration;
+    if (units < clusters) clusters = static_cast<int>(units);
+  }
   {
     KernelScope ks(a.name, s);
-    e = launch_cluster(kernel, clusters, 2, THREADS, (size_t)SMEM, s, mA, mB, mBox, p);
+    e = launch_cluster(kernel, clusters, CLUSTER ? 2 * split : 2, THREADS, (size_t)SMEM, s, mA, mB, mBox, p);
     if (e != cudaSuccess) return e;
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
@@ -916,22 +1038,23 @@ cudaError_t launch(const GroupedArgs& a, int split, cudaStream_t s) {
 
 template <int FORM>
 cudaError_t launch_form(const GroupedArgs& a, cudaStream_t s) {
-  const int split = split_of(FORM, a.G, a.rows, a.N, a.K);
-  const bool f32 = !a.out_bf16 || split > 1;
+  const Plan plan = plan_of(FORM, a.G, a.rows, a.N, a.K);
+  if (plan.cluster) return launch<FORM, true, false, true>(a, plan.split, s);
+  if (plan.split > 1) return launch<FORM, true, false, false>(a, plan.split, s);
   if constexpr (FORM != WGRAD) {
-    if (a.perm && split == 1) return f32 ? launch<FORM, true, true>(a, 1, s) : launch<FORM, false, true>(a, 1, s);
+    if (a.perm) return a.out_bf16 ? launch<FORM, false, true, false>(a, 1, s) : launch<FORM, true, true, false>(a, 1, s);
   }
-  return f32 ? launch<FORM, true, false>(a, split, s) : launch<FORM, false, false>(a, split, s);
+  return a.out_bf16 ? launch<FORM, false, false, false>(a, 1, s) : launch<FORM, true, false, false>(a, 1, s);
 }
 
 }  // namespace
 
 size_t grouped_bytes(int form, int G, int rows, int N, int K) {
-  const int split = split_of(form, G, rows, N, K);
-  if (split == 1) return 0;
+  const Plan plan = plan_of(form, G, rows, N, K);
+  if (plan.split == 1 || plan.cluster) return 0;
   const size_t out = form == GROUPED_WGRAD ? static_cast<size_t>(G) * N * K
                                            : static_cast<size_t>(rows) * (form == GROUPED_FWD ? N : K);
-  return split * out * 4;
+  return plan.split * out * 4;
 }
 
 cudaError_t launch_grouped(const GroupedArgs& a, int form, cudaStream_t s) {
