@@ -254,14 +254,6 @@ struct Shared {
   int *prefix, *row0, *cnt;
 };
 
-// The groups' first rows and row counts, and the prefix of their row tiles.
-__device__ __forceinline__ void scan_groups(const Params& p, int lane, const Shared& sh) {
-  constexpr int CHUNKS = (MAX_GROUPS + 31) / 32;
-  scan_group_rows<CHUNKS, 1>(p.offsets, p.G, p.rows, lane, sh.row0, sh.cnt, sh.prefix, &g_grouped_error);
-  __syncwarp();
-  warp_exclusive_scan<CHUNKS>(p.G, lane, [&](int g) { return (sh.cnt[g] + BN - 1) / BN; }, sh.prefix);
-}
-
 template <int FORM>
 __device__ __forceinline__ Tile decode_any(const Params& p, int unit, const int* prefix, const int* cnt) {
   int cursor = 0;
@@ -370,11 +362,12 @@ __global__ void __launch_bounds__(THREADS, 1)
   }
   if (warp == 0) {
     pdl_wait();
-    scan_groups(p, lane, sh);
-    if (lane == 0) {
-      tma_prefetch_desc(&tmA);
-      tma_prefetch_desc(&tmB);
-    }
+    scan_group_rows<(MAX_GROUPS + 31) / 32, BN>(p.offsets, p.G, p.rows, lane, sh.row0, sh.cnt, sh.prefix, &g_grouped_error);
+  }
+  if (warp == 2 && lane == 0) {
+    tma_prefetch_desc(&tmA);
+    tma_prefetch_desc(&tmB);
+    if (FORM != WGRAD) tma_prefetch_desc(&tmBox);
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),

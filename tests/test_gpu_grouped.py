@@ -183,6 +183,28 @@ def test_ragged_sums_of_many_tiles(lengths, out_type):
         check("wgrad", X, W, offsets, G, rows, N, K, out, out_type)
 
 
+@pytest.mark.parametrize("out_type,accumulate", [(C.BF16, 0), (C.F32, 0), (C.F32, 1)])
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("lengths,N,K", [([0, 3000, 1], 264, 520), ([900, 0, 40, 1500], 520, 1024), ([130], 264, 2048), ([7], 2048, 264),
+                                         ([2, 1, 300, 0, 5], 1032, 1544)])
+def test_few_tiles(form, lengths, N, K, out_type, accumulate):
+    """Sums that are cut into ranges, for groups with many, few and no rows."""
+    offsets = [0]
+    for n in lengths:
+        offsets.append(offsets[-1] + n)
+    G, rows = len(lengths), offsets[-1]
+    X, W = operands(form, rows, N, K, G, seed=15)
+    out = call(form, X, W, offsets, G, rows, N, K, out_type)
+    check(form, X, W, offsets, G, rows, N, K, out, out_type)
+    if accumulate and form == "wgrad":
+        twice = call(form, X, W, offsets, G, rows, N, K, out_type, accumulate=1, into=out.clone())
+        assert torch.equal(twice, out + out)
+    elif form != "wgrad":
+        perm = torch.arange(rows, dtype=torch.int32, device="cuda").flip(0).contiguous()
+        other = call(form, X, W, offsets, G, rows, N, K, out_type, perm=perm)
+        assert torch.equal(other, out.flip(0))
+
+
 @pytest.mark.parametrize("form", FORMS)
 def test_other_groups_values_stay_out(form):
     """Infinities and NaN in one group's rows, and in rows of no group, reach no other group's results."""
