@@ -41,6 +41,7 @@ using namespace tc;
 
 constexpr int PER = 8;        // columns per thread and step: 16 bytes of bf16
 constexpr int MAX_WARPS = 32;
+constexpr int LANES = FP8_BLOCK / PER;  // threads of a block of the quantisation
 
 // Sum over the tpr threads (whole warps) of a row; every thread gets it.  The
 // warps' sums are added in order.
@@ -58,14 +59,35 @@ __device__ __forceinline__ float row_sum(float v, int tpr, float* s_sum) {
   return t;
 }
 
+// Where a quotient's bits 0-19 lie from a tie of e4m3 (ordinary values), times 2^12: 0 .. 10
+// for TIE_UNITS = 5 units of fp32's last place below it to 5 above.
+constexpr uint32_t TIE_UNITS = 5;
+constexpr uint32_t BESIDE_TIE = 2 * TIE_UNITS << 12;
+__device__ __forceinline__ uint32_t beside_tie(float q) { return __float_as_uint(q) * 4096u + ((0x80000u + TIE_UNITS) << 12); }
+// The sign of x = 448 |h w| - tie m decides such a one, m = m1 + m2 the exact largest |h w|:
+// the products' rounding errors are exact fp32 numbers, and what is left of the products,
+// a few units of their last place, is exact too.
+__device__ __forceinline__ float decide_tie(float q, float h, float w, float m1, float m2) {
+  const uint32_t bits = __float_as_uint(q) & 0x7fffffffu;
+  const uint32_t tie_bits = bits + TIE_UNITS - (beside_tie(q) >> 12);
+  const float tie = __uint_as_float(tie_bits);
+  const float p1 = fabsf(h * w), p2 = copysignf(1.0f, h * w) * fmaf(h, w, -(h * w));
+  const float y = 448.0f * p1, x = tie * m1;
+  const float d = (y - x) + (fmaf(448.0f, p1, -y) - fmaf(tie, m1, -x) + (448.0f * p2 - tie * m2));
+  const uint32_t r = d > 0.0f ? tie_bits + 1u : d < 0.0f ? tie_bits - 1u : tie_bits;
+  return __uint_as_float(r | (__float_as_uint(q) & 0x80000000u));
+}
+
 // A chunk of PER columns of a row: y = h rstd w, stored and quantised.  The 16 lanes
 // of a block of 128 columns call it together, `mine` where the chunk is inside the row.
-// h w times 448 over its largest magnitude in the block is the quotient that e4m3 rounds:
-// rstd is in both and leaves no error, and h w's own rounding and the quotient's
-// are carried along (`lost`, `low`), so that the value is rounded to fp32 once.
+// rstd is in a value and in its block's largest alike: what e4m3 rounds is 448 h w over
+// the largest |h w|.  In fp32 that quotient is within 4 units of its last place (2 for the
+// fast division, half each for the two products, the largest and the last product), so
+// where it is further from a tie of e4m3 its rounding is right; a warp that holds another
+// one, one in 400, decides that by exact products.  Returns the block's largest |y|.
 template <typename TX, typename TY>
-__device__ __forceinline__ void finish_chunk(const NormArgs& a, long long row, int c, bool mine, float rstd, const float* h,
-                                             const float* w) {
+__device__ __forceinline__ float finish_chunk(const NormArgs& a, long long row, int c, bool mine, float rstd, const float* h,
+                                              const float* w) {
   if (mine && a.H) store8(static_cast<TX*>(a.H) + row * a.cols + c * PER, h);
   if (mine && a.Y) {
     float y[PER];
@@ -73,20 +95,17 @@ __device__ __forceinline__ void finish_chunk(const NormArgs& a, long long row, i
     for (int j = 0; j < PER; ++j) y[j] = h[j] * rstd * w[j];
     store8(static_cast<TY*>(a.Y) + row * a.cols + c * PER, y);
   }
-  if (!a.Q) return;
-  float p[PER], lost[PER];
+  if (!a.Q) return 0.0f;
+  float q[PER];
   float m = 0.0f;
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
-    p[j] = mine ? h[j] * w[j] : 0.0f;
-    lost[j] = mine ? fmaf(h[j], w[j], -p[j]) : 0.0f;
-    m = fmaxf(m, fabsf(p[j]));
+    q[j] = h[j] * w[j];  // 0 where the chunk is not inside the row
+    m = fmaxf(m, fabsf(q[j]));
   }
 #pragma unroll
-  for (int o = 1; o < FP8_BLOCK / PER; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  const float most = m * rstd;  // the largest |y|
-  Fp8Scale f{__fdiv_rn(most, 448.0f), __fdiv_rn(448.0f, m)};
-  const float low = __fdiv_rn(fmaf(-f.inv, m, 448.0f), m);
+  for (int o = 1; o < LANES; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  float most = m * rstd;
   const bool plain = most >= 0x1p-96f && most < INFINITY && m < 0x1p100f && m > 0x1p-90f;
   if (!__all_sync(0xffffffffu, plain || !mine)) {
     // blocks of zeros or next to them, infinities and NaN: fp8_scale's rule on y itself
@@ -95,23 +114,43 @@ __device__ __forceinline__ void finish_chunk(const NormArgs& a, long long row, i
     for (int j = 0; j < PER; ++j)
       if (mine) z = fmaxf(z, fabsf(h[j] * rstd * w[j]));
 #pragma unroll
-    for (int o = 1; o < FP8_BLOCK / PER; o <<= 1) z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, o));
+    for (int o = 1; o < LANES; o <<= 1) z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, o));
     if (!plain) {
-      f = fp8_scale(z);
+      most = z;
+      const float inv = fp8_scale(z).inv;
 #pragma unroll
-      for (int j = 0; j < PER; ++j) p[j] = h[j] * rstd * w[j] * f.inv;
+      for (int j = 0; j < PER; ++j) q[j] = h[j] * rstd * w[j] * inv;
     }
   }
-  if (!mine) return;
+  uint32_t nearest = 0xffffffffu;
   if (plain) {
+    const float inv = __fdividef(448.0f, m);
 #pragma unroll
-    for (int j = 0; j < PER; ++j) p[j] = fmaf(p[j], f.inv, fmaf(p[j], low, lost[j] * f.inv));
+    for (int j = 0; j < PER; ++j) {
+      q[j] *= inv;
+      nearest = min(nearest, beside_tie(q[j]));
+    }
   }
-  const uint32_t q0 = fp8_pack2(p[0], p[1], 1.0f) | (fp8_pack2(p[2], p[3], 1.0f) << 16);
-  const uint32_t q1 = fp8_pack2(p[4], p[5], 1.0f) | (fp8_pack2(p[6], p[7], 1.0f) << 16);
+  if (__any_sync(0xffffffffu, nearest <= BESIDE_TIE)) {
+    float m2 = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const float p = h[j] * w[j];
+      if (fabsf(p) == m) m2 = fmaxf(m2, copysignf(1.0f, p) * fmaf(h[j], w[j], -p));
+    }
+#pragma unroll
+    for (int o = 1; o < LANES; o <<= 1) m2 = fmaxf(m2, __shfl_xor_sync(0xffffffffu, m2, o));
+    if (nearest <= BESIDE_TIE) {
+#pragma unroll
+      for (int j = 0; j < PER; ++j)
+        if (beside_tie(q[j]) <= BESIDE_TIE) q[j] = decide_tie(q[j], h[j], w[j], m, m2);
+    }
+  }
+  if (!mine) return most;
+  const uint32_t q0 = fp8_pack2(q[0], q[1], 1.0f) | (fp8_pack2(q[2], q[3], 1.0f) << 16);
+  const uint32_t q1 = fp8_pack2(q[4], q[5], 1.0f) | (fp8_pack2(q[6], q[7], 1.0f) << 16);
   *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.Q) + row * a.cols + c * PER) = make_uint2(q0, q1);
-  const int n_kb = (a.cols + FP8_BLOCK - 1) / FP8_BLOCK;
-  if (c % (FP8_BLOCK / PER) == 0) a.scale[row * n_kb + c / (FP8_BLOCK / PER)] = f.scale;
+  return most;
 }
 
 __device__ __forceinline__ float rstd_of(float sum, const NormArgs& a) {
@@ -146,7 +185,8 @@ __global__ void __launch_bounds__(1024) rmsnorm_kernel(const NormArgs a) {
   sum = row_sum(sum, blockDim.x, s_sum);
   const float rstd = rstd_of(sum, a);
   if (c == 0 && a.rstd) a.rstd[row] = rstd;
-  finish_chunk<TX, TY>(a, row, c, mine, rstd, h, w);
+  const float most = finish_chunk<TX, TY>(a, row, c, mine, rstd, h, w);
+  if (a.Q && mine && c % LANES == 0) a.scale[row * ((a.cols + FP8_BLOCK - 1) / FP8_BLOCK) + c / LANES] = fp8_scale(most).scale;
 }
 
 // ------------------------------------------------------------- rows through a ring
@@ -273,6 +313,7 @@ __global__ void __launch_bounds__(RING_THREADS, 1) rmsnorm_ring_kernel(const Nor
     for (int j = 0; j < PER; ++j) w[i][j] = 1.0f;
     if (a.weight && i * g.tpr + t < n_chunks) load8(a.weight + (i * g.tpr + t) * PER, w[i]);
   }
+  const int n_kb = (a.cols + FP8_BLOCK - 1) / FP8_BLOCK;
   int d = 0, turn = 0;
   uint32_t phase = 0;
   volatile int no_abort = 0;
@@ -305,10 +346,17 @@ __global__ void __launch_bounds__(RING_THREADS, 1) rmsnorm_ring_kernel(const Nor
     if (t == 0 && row + g.depth * step < a.rows) fetch(row + g.depth * step, d);
     const float rstd = rstd_of(sum, a);
     if (t == 0 && a.rstd) a.rstd[row] = rstd;
+    // lane i of a block's 16 keeps chunk i's scale: one division for all of them
+    float most = 0.0f;
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
       if (i * g.tpr >= n_chunks) break;  // the whole row
-      finish_chunk<TX, TY>(a, row, i * g.tpr + t, i * g.tpr + t < n_chunks, rstd, h[i], w[i]);
+      const float v = finish_chunk<TX, TY>(a, row, i * g.tpr + t, i * g.tpr + t < n_chunks, rstd, h[i], w[i]);
+      if (t % LANES == i) most = v;
+    }
+    if (a.Q && t % LANES < NCH) {
+      const int c = t % LANES * g.tpr + t / LANES * LANES;  // the block's first chunk
+      if (c < n_chunks) a.scale[row * n_kb + c / LANES] = fp8_scale(most).scale;
     }
     turn ^= 1;
     if (++d == g.depth) {
