@@ -5,8 +5,7 @@
 //
 // h is the fp32 sum: y and its quantisation are taken from it, not from the h
 // that is stored rounded.  y is stored in 16 or 32 bits, and/or quantised to e4m3
-// with a scale per 128 columns by quantize_rows' rule (fp8.cuh), from the fp32
-// value.  With g = dy w and xhat = h rstd the gradient is
+// with a scale per 128 columns by quantize_rows' rule (fp8.cuh).  With g = dy w and xhat = h rstd the gradient is
 //
 //   dx = rstd (g - xhat mean(g xhat)) + dh,   dw = sum over rows of dy xhat.
 //
@@ -18,7 +17,12 @@
 // operand is read once, and H or dx may take an operand's place.  The gradient's
 // threads keep their columns' share of dw over all their rows; a second kernel adds
 // up the CTAs' shares in a fixed order.  Short calls take a CTA per row, without the
-// ring.
+// ring (300 x 4096: 5.4 us, with it 8).
+//
+// Measured: 16384 x 4096 bf16 with residual and 8-bit rows 100 us (6.0 TB/s; with plain
+// loads, a row in registers, 133), its gradient 88 us (6.1 TB/s), fp32 160 us (6.7 TB/s);
+// 16384 x 2048, gradient, 50 us, of which 4 are the second kernel.  Rows stored by bulk
+// copies from the ring were slower (111), as were stores that leave L2 first.
 //
 // Every wait for a row is bounded: one that gives up sets the error word, the team
 // waits for its copies in flight and ends.
