@@ -232,6 +232,14 @@ __device__ __forceinline__ void tmem_ld_16x16_nw(uint32_t taddr, uint32_t* r) {
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
                : "r"(taddr));
 }
+// Waits for the TMEM loads so far; what they brought is used behind it, for the compiler
+// too (a wait alone names no register).
+template <int N>
+__device__ __forceinline__ void tmem_wait_for(uint32_t* r) {
+  tmem_wait();
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+r"(r[i]));
+}
 // Four 8 x 8 matrices of 16-bit elements, stored transposed: thread t names row t % 8 of
 // matrix t / 8 (16 bytes).
 __device__ __forceinline__ void store_4_transposed(uint32_t saddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
@@ -586,7 +594,6 @@ __global__ void __launch_bounds__(THREADS, 1)
     const int q = warp & 3;
     const int part = (warp - FIRST_EPI) >> 2;
     constexpr int NB = BN / 64;  // blocks of a warp
-    using OutT = typename std::conditional<F32, float, __nv_bfloat16>::type;
     uint32_t it = 0;
     int cursor = 0;
     auto load_block = [&](uint32_t lanes, int b, uint32_t* r) {
@@ -641,7 +648,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         uint32_t r[NB][16];
 #pragma unroll
         for (int b = 0; b < NB; ++b) load_block(lanes + (it & 1u) * BN, b, r[b]);
-        tmem_wait();
+        tmem_wait_for<NB * 16>(&r[0][0]);
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -661,7 +668,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         for (int b = 0; b < NB; ++b) {
           uint32_t r[16];
           load_block(lanes + (it & 1u) * BN, b, r);
-          tmem_wait();
+          tmem_wait_for<16>(r);
 #pragma unroll
           for (int i = 0; i < 16; ++i) v[b][i] += __uint_as_float(r[i]);
         }

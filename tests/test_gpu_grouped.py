@@ -109,7 +109,8 @@ def test_small(form, N, K, table):
 
 
 @pytest.mark.parametrize("form", FORMS)
-@pytest.mark.parametrize("rows,N,K", [(1, 4096, 1024), (300, 512, 4096), (5000, 264, 1408), (1027, 3000, 2056)])
+@pytest.mark.parametrize("rows,N,K", [(1, 4096, 1024), (300, 512, 4096), (5000, 264, 1408), (1027, 3000, 2056), (20001, 4104, 2560),
+                                      (2500, 2560, 10248), (2500, 10248, 2560)])
 @pytest.mark.parametrize("out_type", [C.BF16, C.F32])
 def test_one_group(form, rows, N, K, out_type):
     X, W = operands(form, rows, N, K, 1, seed=1)
