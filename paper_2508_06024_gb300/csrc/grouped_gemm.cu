@@ -728,29 +728,40 @@ __global__ void __launch_bounds__(THREADS, 1)
         const uint32_t put = stg + (lane & 7) * 64 + (((lane >> 3) ^ ((lane >> 1) & 3)) * 16);
         const uint32_t get = stg + (lane >> 2) * 64 + (((lane & 3) ^ ((lane >> 3) & 3)) * 16);
         const bool held = col0 + (lane & 3) * 8 < p.cols;
+        // packed at once, which leaves half the registers (16384 rows of 8 experts of 4096 x
+        // 512, forward: 58 us without it, 50 with it)
+        uint32_t w[NB][8];
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) w[b][i] = pack_bf16x2(v[b][2 * i], v[b][2 * i + 1]);
         __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + col0 + (lane & 3) * 8;
         if (FORM == WGRAD) out += static_cast<long long>(t.g) * p.out_rows * p.ldo;
+        const int r0 = part * 16 + (lane >> 2);
+        if (!PERM) out += (first + r0) * p.ldo;
+        const long long step = p.ldo * 8;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
           if ((part + 4 * b) * 16 >= t.n) break;  // the whole warp
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {  // 8 rows each
-            const float* f = v[b] + 4 * k;
-            store_4_transposed(put + (b & 1) * STG_BLOCK + k * 512, pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]),
-                               pack_bf16x2(f[8], f[9]), pack_bf16x2(f[10], f[11]));
-          }
+          for (int k = 0; k < 2; ++k)  // 8 rows each
+            store_4_transposed(put + (b & 1) * STG_BLOCK + k * 512, w[b][2 * k], w[b][2 * k + 1], w[b][2 * k + 4],
+                               w[b][2 * k + 5]);
           __syncwarp();
+          U4 o[2];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int r = (part + 4 * b) * 16 + 8 * h + (lane >> 2);
-            U4 o;
+          for (int h = 0; h < 2; ++h)
             asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                         : "=r"(o.x), "=r"(o.y), "=r"(o.z), "=r"(o.w)
+                         : "=r"(o[h].x), "=r"(o[h].y), "=r"(o[h].z), "=r"(o[h].w)
                          : "r"(get + (b & 1) * STG_BLOCK + h * 512)
                          : "memory");
-            const bool on = held && (PERM ? dst[b][h] >= 0 : r < t.n);
-            const long long d = PERM ? dst[b][h] : first + r;
-            if (on) *reinterpret_cast<U4*>(out + d * p.ldo) = o;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if constexpr (PERM) {
+              if (held && dst[b][h] >= 0) *reinterpret_cast<U4*>(out + dst[b][h] * p.ldo) = o[h];
+            } else {
+              if (held && r0 + 64 * b + 8 * h < t.n) *reinterpret_cast<U4*>(out + (8 * b + h) * step) = o[h];
+            }
           }
         }
         __syncwarp();
