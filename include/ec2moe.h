@@ -27,7 +27,7 @@
  *    the tensor-core kernels are bounded and report through a device error
  *    word that ec2moe_last_device_error reads.
  *  - Calls are thread-safe with respect to each other as long as they do not
- *    share output buffers.
+ *    share output buffers or workspaces.
  */
 #ifndef EC2MOE_H
 #define EC2MOE_H

@@ -7,7 +7,7 @@
 // SiLU'(u) = p (1 + u (1 - p)); GELU(u) = u P(u) with P the normal distribution,
 // GELU'(u) = P(u) + u e^(-u^2 / 2) / sqrt(2 pi).  P is taken from the fitted erfc of the 8-bit
 // experts (2.8e-8 at most, fp8.cuh): erff bound the kernel by its instructions (98304 x
-// 1408 GELU: 169 us, now 118; gradient 256, 208).  The gradient computes h again (the
+// 1408 GELU: 169 us, now 115; gradient 256, 206).  The gradient computes h again (the
 // weights' gradient needs it, and it costs no read) and the gate weight's, the row's sum
 // of dh a.
 //
@@ -60,6 +60,12 @@ __device__ __forceinline__ void widen8(const Raw8<float>& r, float* v) {
 
 __device__ __forceinline__ float sigmoid(float u) { return __fdividef(1.0f, 1.0f + __expf(-u)); }
 
+// P(u), with e = e^(-u^2 / 2).
+__device__ __forceinline__ float normal(float u, float e) {
+  const float tail = 0.5f * erfc_fit(fabsf(u), e);
+  return u < 0.0f ? tail : 1.0f - tail;
+}
+
 // The row's slot, or -1 (reported) where perm names none of the call's rows.
 __device__ __forceinline__ int slot_of(const ActArgs& a, long long row, int t) {
   if (!a.perm) return static_cast<int>(row);
@@ -88,7 +94,7 @@ __global__ void __launch_bounds__(THREADS) activation_kernel(const ActArgs a, in
     load8(u + c, x);
     if (GLU) load8(v + c, y);
 #pragma unroll
-    for (int j = 0; j < PER; ++j) x[j] = GLU ? x[j] * sigmoid(x[j]) * y[j] * w : gelu_fp8out(x[j]) * w;
+    for (int j = 0; j < PER; ++j) x[j] = GLU ? x[j] * sigmoid(x[j]) * y[j] * w : x[j] * normal(x[j], gauss(x[j])) * w;
     store8(h + c, x);
   }
 }
@@ -140,8 +146,7 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 4 : 3) activation_ba
           x[j] = gw * y[j] * (p * (1.0f + x[j] * (1.0f - p)));
           y[j] = gw * s;
         } else {
-          const float e = gauss(x[j]), tail = 0.5f * erfc_fit(fabsf(x[j]), e);
-          const float P = x[j] < 0.0f ? tail : 1.0f - tail, act = x[j] * P;
+          const float e = gauss(x[j]), P = normal(x[j], e), act = x[j] * P;
           sum = fmaf(g[j], act, sum);
           o[j] = act * w;
           x[j] = gw * (P + x[j] * e * 0.3989422804014327f);

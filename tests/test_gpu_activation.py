@@ -125,6 +125,31 @@ def test_large_arguments():
         assert float(H[0, 7]) == 0 and float(du[0, 7]) == 0
 
 
+@pytest.mark.parametrize("glu", [True, False])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_the_gradients_rows_are_the_forwards(glu, dtype):
+    """Bit for bit, infinities and NaN too: u P(u) and u p are inf at inf and NaN (inf times 0) at -inf, in their place only."""
+    rows, cols = 5, 200
+    uv, perm, scale, dh = make(rows, cols, dtype, glu, seed=9)
+    at = {7: float("inf"), 80: float("-inf"), 199: float("nan")}
+    for c, x in at.items():
+        uv[2, c] = x
+    act, ld = C.SWIGLU if glu else C.GELU, uv.shape[1]
+    v = uv[:, cols:] if glu else None
+    if glu:
+        uv[2, cols:2 * cols] = 1.0
+    H, H2, duv = torch.empty(rows, cols, dtype=dtype, device="cuda"), torch.empty_like(dh), torch.zeros_like(uv)
+    C.ec2moe_activation(CODE[dtype], act, rows, cols, ld, uv, v, perm, scale, H)
+    C.ec2moe_activation_backward(CODE[dtype], act, rows, cols, ld, uv, v, perm, scale, dh, duv,
+                                 duv[:, cols:] if glu else None, H2, None)
+    bits = torch.int16 if dtype == BF else torch.int32
+    assert torch.equal(H.nan_to_num(3.0).view(bits), H2.nan_to_num(3.0).view(bits))
+    assert float(H[2, 7]) == float("inf") and bool(H[2, [80, 199]].isnan().all())
+    for x in (H, duv):
+        bad = (~x.isfinite()).nonzero().tolist()
+        assert {r for r, _ in bad} == {2} and {c % cols for _, c in bad} <= set(at)
+
+
 def test_bad_slots_are_skipped_and_reported():
     uv, perm, scale, dh = make(6, 64, BF, True)
     perm = torch.tensor([0, 5, -1, 2, 6, 1], dtype=torch.int32, device="cuda")
