@@ -95,20 +95,24 @@ __device__ __forceinline__ U4 fp8_pack16(const float* v, float inv) {
 // erfc(x / sqrt 2) for x >= 0, with e = e^(-x^2 / 2) given: (c1 t + .. + c6 t^6) e, t = 1 /
 // (1 + 0.4 x / sqrt 2), the form of Abramowitz & Stegun 7.1.26 with one term more, fitted
 // here to the least largest error (Lawson's weights): 2.8e-8.
+constexpr float ERFC_T = 0.4f * 0.70710678118654752f;
+constexpr float ERFC_1 = 0.231922259f, ERFC_2 = 0.16182253f, ERFC_3 = 0.468276749f, ERFC_4 = -0.370911135f,
+                ERFC_5 = 0.709149296f, ERFC_6 = -0.200259726f;
+constexpr float GAUSS = -0.5f * 1.4426950408889634f;  // e^(-u^2 / 2) = 2^(GAUSS u^2)
 __device__ __forceinline__ float erfc_fit(float x, float e) {
   float t;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(fmaf(x, 0.4f * 0.70710678118654752f, 1.0f)));
-  float q = fmaf(t, -0.200259726f, 0.709149296f);
-  q = fmaf(t, q, -0.370911135f);
-  q = fmaf(t, q, 0.468276749f);
-  q = fmaf(t, q, 0.16182253f);
-  q = fmaf(t, q, 0.231922259f);
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(fmaf(x, ERFC_T, 1.0f)));
+  float q = fmaf(t, ERFC_6, ERFC_5);
+  q = fmaf(t, q, ERFC_4);
+  q = fmaf(t, q, ERFC_3);
+  q = fmaf(t, q, ERFC_2);
+  q = fmaf(t, q, ERFC_1);
   return q * t * e;
 }
 // e^(-u^2 / 2)
 __device__ __forceinline__ float gauss(float u) {
   float e;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(u * u * (-0.5f * 1.4426950408889634f)));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(u * u * GAUSS));
   return e;
 }
 // GELU(u) = u Phi(u) = max(u, 0) - |u| erfc(|u| / sqrt 2) / 2 to fp32's own rounding,
