@@ -943,7 +943,7 @@ Plan plan_of(int form, int G, int rows, int N, int K) {
   if (form == WGRAD) {
     tiles = tiles_c * G * ((N + BN - 1) / BN);
     out = static_cast<double>(G) * N * K;
-    n_kb = (rows / G + BK - 1) / BK;
+    n_kb = rows < G ? 1 : (rows / G + BK - 1) / BK;  // fewer rows than groups: those with one have a block
     bytes = 2.0 * rows * (static_cast<double>(N) + K) + 2.0 * out;
   } else {
     tiles = tiles_c * (rows < held * BN ? held : rows / BN + 0.5 * held);
