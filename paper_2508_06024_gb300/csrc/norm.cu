@@ -63,32 +63,52 @@ __device__ __forceinline__ float row_sum(float v, int tpr, float* s_sum) {
   return t;
 }
 
-// Where a quotient's bits 0-19 lie from a tie of e4m3 (ordinary values), times 2^12: 0 .. 10
-// for TIE_UNITS = 5 units of fp32's last place below it to 5 above.
-constexpr uint32_t TIE_UNITS = 5;
+// e4m3's ties.  From 2^-6 on its values have 3 bits behind the leading one, so a quotient at a tie
+// has 0x80000 in its bits 0-19; below, its steps are 2^-9 throughout, as between 2^-6 and 2^-5, so
+// there the same goes for the quotient plus 2^-6.
+constexpr float NORMAL = 0x1p-6f;  // e4m3's least value with a leading one
+__device__ __forceinline__ float subnormal_shift(float q) { return fabsf(q) < NORMAL ? NORMAL : 0.0f; }
+// Where bits 0-19 lie from a tie's, times 2^12: 0 .. 14 for TIE_UNITS = 7 units of the last place below
+// it to 7 above.
+constexpr uint32_t TIE_UNITS = 7;
 constexpr uint32_t BESIDE_TIE = 2 * TIE_UNITS << 12;
-__device__ __forceinline__ uint32_t beside_tie(float q) { return __float_as_uint(q) * 4096u + ((0x80000u + TIE_UNITS) << 12); }
-// The sign of x = 448 |h w| - tie m decides such a one, m = m1 + m2 the exact largest |h w|:
-// the products' rounding errors are exact fp32 numbers, and what is left of the products,
-// a few units of their last place, is exact too.
-__device__ __forceinline__ float decide_tie(float q, float h, float w, float m1, float m2) {
-  const uint32_t bits = __float_as_uint(q) & 0x7fffffffu;
-  const uint32_t tie_bits = bits + TIE_UNITS - (beside_tie(q) >> 12);
-  const float tie = __uint_as_float(tie_bits);
-  const float p1 = fabsf(h * w), p2 = copysignf(1.0f, h * w) * fmaf(h, w, -(h * w));
-  const float y = 448.0f * p1, x = tie * m1;
-  const float d = (y - x) + (fmaf(448.0f, p1, -y) - fmaf(tie, m1, -x) + (448.0f * p2 - tie * m2));
-  const uint32_t r = d > 0.0f ? tie_bits + 1u : d < 0.0f ? tie_bits - 1u : tie_bits;
-  return __uint_as_float(r | (__float_as_uint(q) & 0x80000000u));
+__device__ __forceinline__ uint32_t beside_tie(float z) { return __float_as_uint(z) * 4096u + ((0x80000u + TIE_UNITS) << 12); }
+// v = |a b| as the 24 bits of its fp32 rounding p and the rounding error e, exact in fp32: v 2^(47 - k),
+// k the exponent of p, an integer of 48 bits.
+__device__ __forceinline__ int exponent(float p) { return static_cast<int>(__float_as_uint(p) >> 23) - 127; }
+__device__ __forceinline__ float product_error(float a, float b) {
+  const float p = a * b;
+  return copysignf(1.0f, p) * fmaf(a, b, -p);
+}
+__device__ __forceinline__ long long product_bits(float p, float e) {
+  // 2^(47 - k) in two factors, each within fp32's range
+  const int k = exponent(p);
+  const float part = e * __uint_as_float(static_cast<uint32_t>(127 - k) << 23) * 0x1p47f;
+  return (static_cast<long long>((__float_as_uint(p) & 0x7fffffu) | 0x800000u) << 24) + static_cast<int>(part);
+}
+// A quotient q beside a tie, moved to the side of it where 448 |h w| / most lies, most = m + m_error the
+// block's largest |h w|: the signs of integers of 53 bits at most, 448 = 7 2^6 and a tie having 5 bits.
+__device__ __forceinline__ float decide_tie(float q, float h, float w, float m, float m_error) {
+  const float shift = subnormal_shift(q), z = fabsf(q) + shift;
+  const float tie = __uint_as_float(__float_as_uint(z) + TIE_UNITS - (beside_tie(z) >> 12)) - shift;
+  const float p = fabsf(h * w);
+  const uint32_t bits = __float_as_uint(tie);
+  const int up = exponent(p) - exponent(tie) - exponent(m) + 10;  // 1 to 3: the two are next to each other
+  const long long there = 7 * product_bits(p, product_error(h, w)) << up;
+  const long long at = static_cast<long long>(((bits & 0x7fffffu) | 0x800000u) >> 19) * product_bits(m, m_error);
+  const uint32_t r = there > at ? bits + 1u : there < at ? bits - 1u : bits;
+  return copysignf(__uint_as_float(r), q);
 }
 
 // A chunk of PER columns of a row: y = h rstd w, stored and quantised.  The 16 lanes
 // of a block of 128 columns call it together, `mine` where the chunk is inside the row.
 // rstd is in a value and in its block's largest alike: what e4m3 rounds is 448 h w over
-// the largest |h w|.  In fp32 that quotient is within 4 units of its last place (2 for the
-// fast division, half each for the two products, the largest and the last product), so
-// where it is further from a tie of e4m3 its rounding is right; a warp that holds another
-// one, one in 400, decides that by exact products.  Returns the block's largest |y|.
+// the largest |h w|.  The fp32 quotient is within 7 2^-24 of itself (4 for the fast division's 2 units,
+// one each for the two products, the largest's and the last): beside a tie, whose mantissa is 31/16 at
+// most, 6.8 units of its last place (below 2^-6, shifted: 4).  Where it is further from a tie its
+// rounding is right; a warp that holds another one, one in 270, decides that by exact
+// products (as integers: 64-bit floats took 9 us more for 16384 x 4096).  Returns the
+// block's largest |y|.
 template <typename TX, typename TY>
 __device__ __forceinline__ float finish_chunk(const NormArgs& a, long long row, int c, bool mine, float rstd, const float* h,
                                               const float* w) {
@@ -110,7 +130,7 @@ __device__ __forceinline__ float finish_chunk(const NormArgs& a, long long row, 
 #pragma unroll
   for (int o = 1; o < LANES; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   float most = m * rstd;
-  const bool plain = most >= 0x1p-96f && most < INFINITY && m < 0x1p100f && m > 0x1p-90f;
+  const bool plain = most >= 0x1p-96f && most < INFINITY && m < 0x1p100f && m > 0x1p-80f;
   if (!__all_sync(0xffffffffu, plain || !mine)) {
     // blocks of zeros or next to them, infinities and NaN: fp8_scale's rule on y itself
     float z = 0.0f;
@@ -127,27 +147,35 @@ __device__ __forceinline__ float finish_chunk(const NormArgs& a, long long row, 
     }
   }
   uint32_t nearest = 0xffffffffu;
-  if (plain) {
+  float least = INFINITY;
+  if (plain && mine) {
     const float inv = __fdividef(448.0f, m);
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
       q[j] *= inv;
       nearest = min(nearest, beside_tie(q[j]));
+      least = fminf(least, fabsf(q[j]));
     }
   }
-  if (__any_sync(0xffffffffu, nearest <= BESIDE_TIE)) {
-    float m2 = -INFINITY;
+  // first whether the warp holds one next to a normal tie or any below the normal range, then which
+  if (__any_sync(0xffffffffu, nearest <= BESIDE_TIE || least < NORMAL)) {
+    nearest = 0xffffffffu;
+    if (plain && mine) {
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      const float p = h[j] * w[j];
-      if (fabsf(p) == m) m2 = fmaxf(m2, copysignf(1.0f, p) * fmaf(h[j], w[j], -p));
+      for (int j = 0; j < PER; ++j) nearest = min(nearest, beside_tie(fabsf(q[j]) + subnormal_shift(q[j])));
     }
-#pragma unroll
-    for (int o = 1; o < LANES; o <<= 1) m2 = fmaxf(m2, __shfl_xor_sync(0xffffffffu, m2, o));
-    if (nearest <= BESIDE_TIE) {
+    if (__any_sync(0xffffffffu, nearest <= BESIDE_TIE)) {
+      float m_error = -INFINITY;  // of the largest of those that round to m
 #pragma unroll
       for (int j = 0; j < PER; ++j)
-        if (beside_tie(q[j]) <= BESIDE_TIE) q[j] = decide_tie(q[j], h[j], w[j], m, m2);
+        if (fabsf(h[j] * w[j]) == m) m_error = fmaxf(m_error, product_error(h[j], w[j]));
+#pragma unroll
+      for (int o = 1; o < LANES; o <<= 1) m_error = fmaxf(m_error, __shfl_xor_sync(0xffffffffu, m_error, o));
+      if (nearest <= BESIDE_TIE) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+          if (beside_tie(fabsf(q[j]) + subnormal_shift(q[j])) <= BESIDE_TIE) q[j] = decide_tie(q[j], h[j], w[j], m, m_error);
+      }
     }
   }
   if (!mine) return most;
