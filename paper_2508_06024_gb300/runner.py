@@ -267,6 +267,8 @@ class TrainBlockRun:
         need = [C.ec2moe_route_workspace_size(self.desc), C.ec2moe_rmsnorm_backward_workspace_size(T, d)]
         need += [C.ec2moe_grouped_gemm_workspace_size(*s) for s in sizes]
         self.workspace = empty(max(16, *need), dtype=torch.uint8)
+        # the joined rows: calls may run on any stream, and nothing orders those behind this one
+        torch.cuda.current_stream().synchronize()
 
     # the three products of rows X [rows, K] and weights B [G, N, K], their gradients' names as in the header
     def _product(self, G, X, offsets, B, perm, out, stream):
