@@ -539,7 +539,8 @@ ec2moe_status ec2moe_rmsnorm_backward(int32_t dtype, int32_t y_dtype, int32_t ro
  *  row_scale  fp32 [rows] (topk_w of ec2moe_gate), or NULL: 1
  *  H          out [rows, cols], dense
  * (Eq. 1's factor G(x)_i, applied before the linear down projection instead of behind
- * it.)  cols is a multiple of 8.  A perm entry outside [0, rows) leaves its row as it
+ * it.)  cols is a multiple of 8, at most 2^31 - 2049 (more return
+ * EC2MOE_ERR_UNSUPPORTED).  A perm entry outside [0, rows) leaves its row as it
  * was and ec2moe_last_device_error then reports EC2MOE_ERR_INVALID_ARG.  No rows is a
  * no-op. */
 ec2moe_status ec2moe_activation(int32_t dtype, int32_t act, int32_t rows, int32_t cols, int64_t ld, const void* U,

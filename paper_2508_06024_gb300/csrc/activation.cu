@@ -30,6 +30,7 @@ namespace {
 
 constexpr int PER = 8;
 constexpr int THREADS = 256;
+static_assert(ACT_MAX_COLS <= 0x7fffffff - THREADS * PER, "the step behind the last column");
 
 // 8 elements as they lie in memory: fetched ahead, widened when they are used.
 template <typename T>

@@ -1437,6 +1437,7 @@ ec2moe_status ec2moe_activation(int32_t dtype, int32_t act, int32_t rows, int32_
   ec2moe_status st = check_rows(dtype, rows, cols, ld);
   if (st != EC2MOE_OK) return st;
   if (act != EC2MOE_GELU && act != EC2MOE_SWIGLU) return EC2MOE_ERR_INVALID_ARG;
+  if (cols > ACT_MAX_COLS) return EC2MOE_ERR_UNSUPPORTED;
   if (rows == 0) return EC2MOE_OK;
   EC2MOE_REQUIRE_PTR(U);
   EC2MOE_REQUIRE_PTR(H);
@@ -1462,6 +1463,7 @@ ec2moe_status ec2moe_activation_backward(int32_t dtype, int32_t act, int32_t row
   ec2moe_status st = check_rows(dtype, rows, cols, ld);
   if (st != EC2MOE_OK) return st;
   if (act != EC2MOE_GELU && act != EC2MOE_SWIGLU) return EC2MOE_ERR_INVALID_ARG;
+  if (cols > ACT_MAX_COLS) return EC2MOE_ERR_UNSUPPORTED;
   if (rows == 0) return EC2MOE_OK;
   EC2MOE_REQUIRE_PTR(U);
   EC2MOE_REQUIRE_PTR(dH);

@@ -410,6 +410,8 @@ struct ActArgs {
   void* H;                // [rows, cols] dense; gradient: nullptr: not wanted
   float* d_row_scale;     // gradient: by slot, nullptr: not wanted
 };
+// 32-bit column indexes up to the step behind a row's last column, of 256 threads of 8
+constexpr int ACT_MAX_COLS = 0x7fffffff - 2048;
 cudaError_t launch_activation(const ActArgs& a, bool bf16, bool glu, bool back, cudaStream_t s);
 // Reads and clears the activation's device error word (synchronous): nonzero when
 // a slot outside the call's rows was skipped.
