@@ -144,6 +144,8 @@ class Fp8LayerRun:
 
     def forward(self, X: Optional[torch.Tensor] = None, stream=None,
                 residual: Optional[torch.Tensor] = None) -> torch.Tensor:
+        if residual is not None and self.norm_weight is None:
+            raise ValueError("a residual is added in front of a norm, and this layer has none")
         t, cfg, desc = self.inp, self.cfg, self.desc
         ws, n_ws = self.workspace, self.workspace.numel()
         X = t["X"] if X is None else X
@@ -174,7 +176,11 @@ class Fp8LayerRun:
         return self.Y
 
     def balance(self, X: Optional[torch.Tensor] = None, coef: float = 1.0, stream=None) -> torch.Tensor:
-        """The balance loss of the gate on the batch that ``forward`` routed; counts, d_logits and d_bias with it."""
+        """The balance loss of the gate on the batch that ``forward`` routed; counts, d_logits and d_bias with it.
+
+        X is what the gate read of that batch; with a norm those are the rows that ``forward`` normed, and no X is taken."""
+        if X is not None and self.norm_weight is not None:
+            raise ValueError("the gate of a normed layer read the rows that forward normed, not X")
         t, ws = self.inp, self.workspace
         X = self.Xn if self.norm_weight is not None else t["X"] if X is None else X
         C.ec2moe_gate_logits(self.desc, X, t["W_local"], t["b_local"], t["W_global"], t["b_global"], self.logits, ws,
@@ -183,8 +189,10 @@ class Fp8LayerRun:
                               None, self.loss, self.counts, self.d_logits, self.d_bias, ws, ws.numel(), stream)
         return self.loss
 
-    def rebalance(self, steps: int, rate: float) -> list:
-        """`steps` gradient steps of the gate's biases towards even loads on this batch; the losses before each.
+    def rebalance(self, steps: int, rate: float, X: Optional[torch.Tensor] = None,
+                  residual: Optional[torch.Tensor] = None) -> list:
+        """`steps` gradient steps of the gate's biases towards even loads on this batch (``forward``'s X and residual); the
+        losses before each.
 
         A device's mask takes experts away from a gate that was trained with all of
         them; its biases are E + K numbers that can follow the mask."""
@@ -194,8 +202,8 @@ class Fp8LayerRun:
             self.inp["b_global"] = self.inp["b_global"].clone()
         losses = []
         for _ in range(steps):
-            self.forward()
-            losses.append(float(self.balance()))
+            self.forward(X, residual=residual)
+            losses.append(float(self.balance(X if self.norm_weight is None else None)))
             self.inp["b_local"] -= rate * self.d_bias[:E]
             if self.cfg.n_groups > 1:
                 self.inp["b_global"] -= rate * self.d_bias[E:]
