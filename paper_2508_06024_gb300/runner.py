@@ -27,6 +27,21 @@ def weights_for(inp: Dict[str, Optional[torch.Tensor]]) -> C.LayerWeights:
                           V_dec=inp.get("V_dec"))
 
 
+def _check_norm_weight(cfg: LayerConfig, w: torch.Tensor) -> None:
+    if w.dtype != torch.float32 or w.numel() != cfg.d or not w.is_contiguous():
+        raise ValueError(f"a norm's weight is dense fp32 [{cfg.d}], not {w.dtype} {tuple(w.shape)} of strides {w.stride()}")
+
+
+def _check_rows(cfg: LayerConfig, device: torch.device, **rows: Optional[torch.Tensor]) -> None:
+    """The kernels are given addresses alone: rows of another type, number, order or device would be read as if they were
+    dense ones (an expanded gradient beyond its end)."""
+    for name, t in rows.items():
+        if t is not None and (t.dtype != cfg.torch_dtype or t.numel() != cfg.T * cfg.d or not t.is_contiguous()
+                              or t.device != device):
+            raise ValueError(f"{name} is dense {cfg.torch_dtype} [{cfg.T}, {cfg.d}] on {device}, not {t.dtype} "
+                             f"{tuple(t.shape)} of strides {t.stride()} on {t.device}")
+
+
 class LayerRun:
     """Output and workspace buffers of one layer shape on one device."""
 
@@ -81,6 +96,8 @@ class Fp8LayerRun:
 
     def __init__(self, cfg: LayerConfig, inp: Dict[str, Optional[torch.Tensor]], device="cuda",
                  norm_weight: Optional[torch.Tensor] = None, eps: float = 1e-5):
+        if norm_weight is not None:
+            _check_norm_weight(cfg, norm_weight)
         self.cfg = cfg
         self.inp = dict(inp)
         self.desc = desc_for(cfg)
@@ -150,6 +167,7 @@ class Fp8LayerRun:
         ws, n_ws = self.workspace, self.workspace.numel()
         X = t["X"] if X is None else X
         if self.norm_weight is not None:
+            _check_rows(cfg, self.Y.device, X=X, residual=residual)
             q, s = (self.Xn8, self.Xn8_s) if self.shared8 else (None, None)
             C.ec2moe_rmsnorm(cfg.dtype, cfg.dtype, cfg.T, cfg.d, cfg.d, X, residual, self.norm_weight, self.eps, self.H, None,
                              self.Xn, q, s, stream)
@@ -231,6 +249,7 @@ class TrainBlockRun:
                  eps: float = 1e-5, device="cuda"):
         if cfg.dtype != C.BF16:
             raise ValueError("the grouped products take bf16 operands")
+        _check_norm_weight(cfg, norm_weight)
         self.cfg, self.inp, self.norm_weight, self.eps = cfg, dict(inp), norm_weight, eps
         self.desc = desc_for(cfg)
         self.mask = C.host_mask(inp["mask"].to("cpu"))
@@ -305,6 +324,7 @@ class TrainBlockRun:
         """(H, Y): the residual stream behind X's addition, and the layer's output on its norm."""
         t, cfg, desc, ws = self.inp, self.cfg, self.desc, self.workspace
         X = t["X"] if X is None else X
+        _check_rows(cfg, self.Y.device, X=X, residual=residual)
         C.ec2moe_rmsnorm(C.BF16, C.BF16, cfg.T, cfg.d, cfg.d, X, residual, self.norm_weight, self.eps, self.H, self.rstd, self.Xn,
                          None, None, stream)
         C.ec2moe_gate(desc, self.Xn, t["W_local"], t["b_local"], t["W_global"], t["b_global"], self.mask, self.topk_idx,
@@ -330,6 +350,7 @@ class TrainBlockRun:
     def backward(self, dY: torch.Tensor, dH: Optional[torch.Tensor] = None, accumulate: int = 0, stream=None) -> torch.Tensor:
         """dX from the gradients that arrive at Y and (the blocks behind) at H; call it after ``forward``."""
         t, cfg, desc, ws, g = self.inp, self.cfg, self.desc, self.workspace, self.grads
+        _check_rows(cfg, self.Y.device, dY=dY, dH=dH)
         # the combine's: every slot of a token gets the token's row, here in expert order
         C.ec2moe_route(desc, self.topk_idx, self.counts, self.offsets, self.perm, self.inv_perm, dY, cfg.d, self.dYp, ws,
                        ws.numel(), stream)
