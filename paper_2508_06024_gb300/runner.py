@@ -242,7 +242,8 @@ class TrainBlockRun:
     residual (one sum, ``dX``), of the norm's weight, of the experts', shared experts'
     and codec's weights (fp32, ``grads``; ``accumulate`` adds to them), and of the gate
     weights of Top-k (``d_topk_w``, where the gate's own gradient starts: it is not carried
-    on into the gate rows and X here).
+    on into the gate rows and X here, so ``dX`` is without the gate's path).  ``params`` has the
+    tensors that the gradients are of.
     """
 
     def __init__(self, cfg: LayerConfig, inp: Dict[str, Optional[torch.Tensor]], norm_weight: torch.Tensor,
@@ -297,6 +298,19 @@ class TrainBlockRun:
         # the joined rows: calls may run on any stream, and nothing orders those behind this one
         torch.cuda.current_stream().synchronize()
 
+    @property
+    def params(self) -> Dict[str, torch.Tensor]:
+        """The tensors that every call reads, under the names of ``grads``: an optimiser updates these, in place.
+
+        They are the tensors that the constructor was given but for ``up`` and ``ups`` of SwiGLU, which hold W1's rows with
+        W3's behind them: copies, so a later change of W1 or W3 is not seen."""
+        p = {"norm": self.norm_weight, "up": self.up, "W2": self.inp["W2"]}
+        if self.cfg.n_shared:
+            p["ups"], p["W2s"] = self.ups, self.inp["W2s"]
+        if self.cfg.r:
+            p["V_enc"], p["V_dec"] = self.inp["V_enc"], self.inp["V_dec"]
+        return p
+
     # the three products of rows X [rows, K] and weights B [G, N, K], their gradients' names as in the header
     def _product(self, G, X, offsets, B, perm, out, stream):
         ws, (rows, K), N = self.workspace, X.shape, B.shape[-2]
@@ -348,7 +362,8 @@ class TrainBlockRun:
         return self.H, self.Y
 
     def backward(self, dY: torch.Tensor, dH: Optional[torch.Tensor] = None, accumulate: int = 0, stream=None) -> torch.Tensor:
-        """dX from the gradients that arrive at Y and (the blocks behind) at H; call it after ``forward``."""
+        """dX (without the gate's path) from the gradients that arrive at Y and (the blocks behind) at H; call it after
+        ``forward``."""
         t, cfg, desc, ws, g = self.inp, self.cfg, self.desc, self.workspace, self.grads
         _check_rows(cfg, self.Y.device, dY=dY, dH=dH)
         # the combine's: every slot of a token gets the token's row, here in expert order
