@@ -542,7 +542,11 @@ ec2moe_status ec2moe_rmsnorm_backward(int32_t dtype, int32_t y_dtype, int32_t ro
  * it.)  cols is a multiple of 8, at most 2^31 - 2049 (more return
  * EC2MOE_ERR_UNSUPPORTED).  A perm entry outside [0, rows) leaves its row as it
  * was and ec2moe_last_device_error then reports EC2MOE_ERR_INVALID_ARG.  No rows is a
- * no-op. */
+ * no-op.
+ * Accuracy of fp32 rows: SwiGLU within 10 2^-24 of itself where e^-U is finite (U > -88; 0 below), its
+ * derivative in U within 18 2^-24 of SiLU(U)/U (1 + |U|) V; GELU within 2.5e-7 and 2^-23 of itself, its derivative
+ * within 7e-7: absolute bounds, which leave few digits of values below U = -4.  bf16 rows have
+ * SwiGLU within 2e-6 of itself for |U| <= 12 (fast exponentials) before it is rounded, and the same GELU. */
 ec2moe_status ec2moe_activation(int32_t dtype, int32_t act, int32_t rows, int32_t cols, int64_t ld, const void* U,
                                 const void* V, const int32_t* perm, const float* row_scale, void* H,
                                 ec2moe_stream_t stream);
