@@ -282,6 +282,7 @@ __device__ __forceinline__ void join_ranges(const Params& p, const Tile& t, cons
   const int warp = (threadIdx.x >> 5) - FIRST_EPI, lane = threadIdx.x & 31;
   const int piece = static_cast<int>(cta >> 1), share = (t.n + p.split - 1) / p.split;
   const int end = min(t.n, (piece + 1) * share);
+  if (FORM == WGRAD && p.accumulate && t.len == 0) return;  // as it was, the sign of a zero too
   const int col = (t.c * 2 + static_cast<int>(cta & 1u)) * BM + lane * 4;
   uint32_t from[MAX_PAIRS];
 #pragma unroll
