@@ -506,7 +506,10 @@ ec2moe_status ec2moe_balance_loss(const ec2moe_layer_desc* desc, const float* lo
  * One output at least.  cols is a multiple of 8 (with Q of 16), at most 16384 (more
  * return EC2MOE_ERR_UNSUPPORTED).  The squares are summed in fp32: where that sum
  * overflows y is 0, as it is for a row with an infinity, whose infinite elements become NaN;
- * a NaN makes its row NaN.  No rows is a no-op. */
+ * a NaN makes its row NaN.  Squares below 2^-150 count as 0: with eps = 0 a row of zeros
+ * is NaN, and one of such values infinite.  Q is rounded from the exact quotient where a
+ * block's largest |h * weight| is between 2^-80 and 2^100, else from y in fp32.  No rows is
+ * a no-op. */
 ec2moe_status ec2moe_rmsnorm(int32_t dtype, int32_t y_dtype, int32_t rows, int32_t cols, int64_t ld, const void* X,
                              const void* residual, const float* weight, float eps, void* H, float* rstd, void* Y,
                              void* Q, float* scale, ec2moe_stream_t stream);
@@ -543,10 +546,11 @@ ec2moe_status ec2moe_rmsnorm_backward(int32_t dtype, int32_t y_dtype, int32_t ro
  * EC2MOE_ERR_UNSUPPORTED).  A perm entry outside [0, rows) leaves its row as it
  * was and ec2moe_last_device_error then reports EC2MOE_ERR_INVALID_ARG.  No rows is a
  * no-op.
- * Accuracy of fp32 rows: SwiGLU within 10 2^-24 of itself where e^-U is finite (U > -88; 0 below), its
- * derivative in U within 18 2^-24 of SiLU(U)/U (1 + |U|) V; GELU within 2.5e-7 and 2^-23 of itself, its derivative
- * within 7e-7: absolute bounds, which leave few digits of values below U = -4.  bf16 rows have
- * SwiGLU within 2e-6 of itself for |U| <= 12 (fast exponentials) before it is rounded, and the same GELU. */
+ * Accuracy of fp32 rows: SwiGLU within 10 2^-24 of itself where e^-U is finite (U > -88;
+ * 0 below), its derivative in U within 18 2^-24 of |V| (1 + |U|) / (1 + e^-U); GELU within
+ * 2.5e-7 and 2^-23 of itself, its derivative within 7e-7: absolute bounds, which leave few
+ * digits of values below U = -4.  bf16 rows have SwiGLU within 2e-6 of itself for |U| <= 12
+ * (fast exponentials) before it is rounded, and the same GELU. */
 ec2moe_status ec2moe_activation(int32_t dtype, int32_t act, int32_t rows, int32_t cols, int64_t ld, const void* U,
                                 const void* V, const int32_t* perm, const float* row_scale, void* H,
                                 ec2moe_stream_t stream);
@@ -558,7 +562,8 @@ ec2moe_status ec2moe_activation(int32_t dtype, int32_t act, int32_t rows, int32_
  *  H            out, dense, or NULL: the forward's H again (the weights' gradient needs
  *               it); may be dH itself
  *  d_row_scale  out fp32 [rows], or NULL
- * Rows with a perm entry out of range are skipped and reported as above. */
+ * Rows with a perm entry out of range are skipped and reported as above; the others' entries
+ * differ (two rows of one slot would both write its d_row_scale). */
 ec2moe_status ec2moe_activation_backward(int32_t dtype, int32_t act, int32_t rows, int32_t cols, int64_t ld,
                                          const void* U, const void* V, const int32_t* perm, const float* row_scale,
                                          const void* dH, void* dU, void* dV, void* H, float* d_row_scale,

@@ -13,7 +13,8 @@
 //
 // Bounded by HBM.  A row is walked by `tpr` threads (whole warps), 8 columns each
 // at a time.  SwiGLU, 98304 x 1408 bf16: 124 us (6.7 TB/s), gradient 270 us (6.1 TB/s);
-// 1554 x 14336, gradient: 47 us (5.7 TB/s; 3.4 waves of CTAs of one row each).
+// 1554 x 14336, gradient: 47 us (5.7 TB/s; 2.6 waves of CTAs of one row each, four to an SM).
+// GELU is bound by its instructions (floors of 82 and 163).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 

@@ -44,8 +44,9 @@
 //
 // What bounds it: the tensor pipe for long sums and many rows, 91% busy (forward) and 90%
 // (weights) of a 4096-row capture with 2 experts of 14336 x 4096; 16384 rows of 8 of them
-// take 990, 1005 and 965 us (forward, rows' gradient, weights' gradient; 1.95, 1.91 and
-// 1.99 PFLOP/s) before the power cap, about 1200 under it.  With a few rows per expert the
+// take 1163, 1200 and 1240 us back to back, under the power cap (forward, rows' gradient,
+// weights' gradient; 1.65, 1.60 and 1.55 PFLOP/s), one call on a rested card 1052, 1109 and
+// 1145 (1.83, 1.74 and 1.68).  With a few rows per expert the
 // weights' bytes (32 rows of these experts: 142 us, 6.6 TB/s), for their gradient the
 // result's (256 rows: 175 us, 5.4 TB/s; fp32 332 us, 5.7).  Short calls have about 6 us of
 // launch, prologue and hand-overs around their blocks.
