@@ -27,9 +27,10 @@ def weights_for(inp: Dict[str, Optional[torch.Tensor]]) -> C.LayerWeights:
                           V_dec=inp.get("V_dec"))
 
 
-def _check_norm_weight(cfg: LayerConfig, w: torch.Tensor) -> None:
-    if w.dtype != torch.float32 or w.numel() != cfg.d or not w.is_contiguous():
-        raise ValueError(f"a norm's weight is dense fp32 [{cfg.d}], not {w.dtype} {tuple(w.shape)} of strides {w.stride()}")
+def _check_norm_weight(cfg: LayerConfig, device, w: torch.Tensor) -> None:
+    if w.dtype != torch.float32 or w.numel() != cfg.d or not w.is_contiguous() or w.device.type != torch.device(device).type:
+        raise ValueError(f"a norm's weight is dense fp32 [{cfg.d}] on {device}, not {w.dtype} {tuple(w.shape)} of strides "
+                         f"{w.stride()} on {w.device}")
 
 
 def _check_rows(cfg: LayerConfig, device: torch.device, **rows: Optional[torch.Tensor]) -> None:
@@ -97,7 +98,7 @@ class Fp8LayerRun:
     def __init__(self, cfg: LayerConfig, inp: Dict[str, Optional[torch.Tensor]], device="cuda",
                  norm_weight: Optional[torch.Tensor] = None, eps: float = 1e-5):
         if norm_weight is not None:
-            _check_norm_weight(cfg, norm_weight)
+            _check_norm_weight(cfg, device, norm_weight)
         self.cfg = cfg
         self.inp = dict(inp)
         self.desc = desc_for(cfg)
@@ -250,7 +251,7 @@ class TrainBlockRun:
                  eps: float = 1e-5, device="cuda"):
         if cfg.dtype != C.BF16:
             raise ValueError("the grouped products take bf16 operands")
-        _check_norm_weight(cfg, norm_weight)
+        _check_norm_weight(cfg, device, norm_weight)
         self.cfg, self.inp, self.norm_weight, self.eps = cfg, dict(inp), norm_weight, eps
         self.desc = desc_for(cfg)
         self.mask = C.host_mask(inp["mask"].to("cpu"))

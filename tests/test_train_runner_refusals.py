@@ -54,3 +54,9 @@ def test_rows_that_are_not_dense(rows):
                  lambda: block.backward(GOOD, rows), lambda: layer.forward(rows), lambda: layer.forward(residual=rows)):
         with pytest.raises(ValueError, match="is dense"):
             call()
+
+
+@pytest.mark.parametrize("cls", [runner.Fp8LayerRun, runner.TrainBlockRun])
+def test_a_norm_weight_in_host_memory(cls):
+    with pytest.raises(ValueError, match="on cuda"):
+        cls(CFG, {}, norm_weight=torch.ones(64))
